@@ -20,4 +20,4 @@ from .attention import (  # noqa: F401
     probabilities,
     merge_partials,
 )
-from . import kda  # noqa: F401,E402
+from . import kda, q4  # noqa: F401,E402

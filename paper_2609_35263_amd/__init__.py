@@ -1,8 +1,9 @@
-"""Chunked-prefill attention over a paged KV cache, and chunked prefill of a KDA (gated
-delta-rule) layer with recurrent-state snapshots, on AMD MI355X (gfx950).
+"""Chunked-prefill attention over a paged KV cache of bf16 or of 4-bit values, and chunked prefill of KDA
+(gated delta-rule) layers and of linear-attention layers with a decay for each head, with recurrent-state
+snapshots, on AMD MI355X (gfx950).
 
-Thin Python binding of libwavepp_attn.so (C ABI declared in include/wavepp_attn.h and
-include/wavepp_kda.h).  Every step of
+Thin Python binding of libwavepp_attn.so (C ABI declared in include/wavepp_attn.h, include/wavepp_q4.h,
+include/wavepp_kda.h and include/wavepp_lin.h).  Every step of
 the computation runs in the library's HIP kernels; this module only marshals arguments: torch
 tensors are passed as device pointers, the stream is torch's current HIP stream.
 
@@ -12,6 +13,13 @@ Per wave:
     plan_upload(p, ws)                  # enqueue the metadata copy
     append_kv(p, k_new, v_new, k_pool, v_pool, ws)
     chunked_prefill(p, q, k_pool, v_pool, out, lse, ws)
+
+Per wave over 4-bit pages, single tokens (decoding) included:
+    p = q4_plan(...)                    # as plan(...)
+    ws = new_workspace(p)
+    plan_upload(p, ws)
+    q4_append_kv(p, k_new, v_new, k_pool, v_pool, ws)        # pools from q4_new_pool
+    q4_chunked_prefill(p, q, k_pool, v_pool, out, lse, ws)
 
 Per wave of a KDA layer:
     kp = kda_plan(...)                  # host: validate chunk lengths and snapshot slots
@@ -36,6 +44,10 @@ EXPORTED_SYMBOLS = [
     "wavepp_attn_plan_upload", "wavepp_attn_append_kv", "wavepp_attn_chunked_prefill", "wavepp_plan_destroy",
     "wavepp_status_string", "wavepp_last_error", "wavepp_attn_chunked_prefill_noalloc",
 ]
+Q4_SYMBOLS = [
+    "wavepp_q4_page_bytes", "wavepp_q4_plan", "wavepp_q4_append_kv", "wavepp_q4_read_kv", "wavepp_q4_chunked_prefill",
+]
+EXPORTED_SYMBOLS += Q4_SYMBOLS
 MPU_SYMBOLS = [
     "wavepp_mpu_budget_ladder", "wavepp_mpu_create", "wavepp_mpu_admit", "wavepp_mpu_plan", "wavepp_mpu_commit",
     "wavepp_mpu_retire", "wavepp_mpu_get_state", "wavepp_mpu_destroy",
@@ -136,6 +148,15 @@ def load_library(path: str = None) -> ctypes.CDLL:
     lib.wavepp_attn_chunked_prefill.restype = ctypes.c_int
     lib.wavepp_attn_chunked_prefill_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.wavepp_attn_chunked_prefill_noalloc.restype = ctypes.c_int
+    lib.wavepp_q4_page_bytes.argtypes = [i32, i32]
+    lib.wavepp_q4_page_bytes.restype = sz
+    lib.wavepp_q4_plan.argtypes = lib.wavepp_attn_plan.argtypes
+    lib.wavepp_q4_plan.restype = ctypes.c_int
+    for name in ("wavepp_q4_append_kv", "wavepp_q4_read_kv"):
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+        getattr(lib, name).restype = ctypes.c_int
+    lib.wavepp_q4_chunked_prefill.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.wavepp_q4_chunked_prefill.restype = ctypes.c_int
     lib.wavepp_plan_destroy.argtypes = [vp]
     lib.wavepp_plan_destroy.restype = None
     lib.wavepp_status_string.argtypes = [ctypes.c_int]
@@ -234,8 +255,8 @@ class Plan:
             pass
 
 
-def plan(*, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
-         prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0) -> Plan:
+def _plan(entry, *, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
+          prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0) -> Plan:
     lib = load_library()
     prefix = np.ascontiguousarray(prefix_lens, dtype=np.int32)
     chunk = np.ascontiguousarray(chunk_lens, dtype=np.int32)
@@ -248,11 +269,19 @@ def plan(*, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_p
                    float(softmax_scale))
     batch = _Batch(prefix.shape[0], prefix.ctypes.data, chunk.ctypes.data, bt.ctypes.data, bt.shape[1])
     out = ctypes.c_void_p()
-    _check(lib.wavepp_attn_plan(ctypes.byref(shape), ctypes.byref(batch), int(max_splits), ctypes.byref(out)))
+    _check(getattr(lib, entry)(ctypes.byref(shape), ctypes.byref(batch), int(max_splits), ctypes.byref(out)))
     return Plan(out.value, dict(num_q_heads=num_q_heads, num_kv_heads=num_kv_heads, head_dim_qk=head_dim_qk,
                                 head_dim_v=head_dim_v, page_size=page_size, num_pages=num_pages,
                                 kv_shared=bool(kv_shared), softmax_scale=float(softmax_scale),
                                 total_tokens=int(np.add.reduce(chunk))))
+
+
+def plan(*, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
+         prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0) -> Plan:
+    return _plan("wavepp_attn_plan", num_q_heads=num_q_heads, num_kv_heads=num_kv_heads, head_dim_qk=head_dim_qk,
+                 head_dim_v=head_dim_v, page_size=page_size, num_pages=num_pages, softmax_scale=softmax_scale,
+                 prefix_lens=prefix_lens, chunk_lens=chunk_lens, block_table=block_table, kv_shared=kv_shared,
+                 max_splits=max_splits)
 
 
 def plan_for(spec, max_splits=0) -> Plan:
@@ -286,6 +315,20 @@ def _stream(stream):
     if stream is None:
         import torch
         stream = torch.cuda.current_stream()
+    return stream.cuda_stream
+
+
+def _stream_for(stream, *tensors):
+    """The stream of a call whose buffers all have to be on the current device, which is where it launches."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream()
+    here = torch.cuda.current_device()
+    if stream.device.index != here:
+        raise ValueError(f"the stream is of {stream.device}, the current device is {here}")
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a buffer is on {t.device}, the current device is {here}")
     return stream.cuda_stream
 
 
@@ -379,6 +422,97 @@ def chunked_prefill_noalloc(p: Plan, q, k_pool, v_pool, out, lse, k_new=None, v_
     _check(load_library().wavepp_attn_chunked_prefill_noalloc(
         p.handle, _ptr(q, bf, "q"), _ptr(k_new, bf, "k_new"), _ptr(v_new, bf, "v_new"), _ptr(k_pool, bf, "k_pool"),
         _ptr(v_pool, bf, "v_pool"), _ptr(out, bf, "out"), _ptr(lse, f32, "lse"), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# 4-bit paged cache
+# ------------------------------------------------------------------------------------------------
+
+def q4_page_bytes(head_dim, page_size) -> int:
+    """Bytes of one page of one KV head: 17/32 a value."""
+    n = int(load_library().wavepp_q4_page_bytes(int(head_dim), int(page_size)))
+    if not n:
+        raise ValueError(f"a 4-bit cache has head dims 64 and 128 and pages of 16 and 64 tokens, not {head_dim}, {page_size}")
+    return n
+
+
+def q4_new_pool(num_pages, num_kv_heads, head_dim, page_size, device=None):
+    """A pool of 4-bit pages, K's or V's, all values zero."""
+    import torch
+    return torch.zeros((num_pages, num_kv_heads, q4_page_bytes(head_dim, page_size)), dtype=torch.uint8,
+                       device=device or "cuda")
+
+
+def q4_plan(*, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
+            prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0) -> Plan:
+    """plan() for a wave over 4-bit pages (plan_upload and new_workspace take it too)."""
+    p = _plan("wavepp_q4_plan", num_q_heads=num_q_heads, num_kv_heads=num_kv_heads, head_dim_qk=head_dim_qk,
+              head_dim_v=head_dim_v, page_size=page_size, num_pages=num_pages, softmax_scale=softmax_scale,
+              prefix_lens=prefix_lens, chunk_lens=chunk_lens, block_table=block_table, kv_shared=kv_shared,
+              max_splits=max_splits)
+    p._buffers = {**_attn_shapes(p), "pool": (int(num_pages), int(num_kv_heads), q4_page_bytes(head_dim_qk, page_size))}
+    return p
+
+
+def q4_plan_for(spec, max_splits=0) -> Plan:
+    """plan_for() for a wave over 4-bit pages."""
+    return q4_plan(num_q_heads=spec.num_q_heads, num_kv_heads=spec.num_kv_heads, head_dim_qk=spec.head_dim_qk,
+                   head_dim_v=spec.head_dim_v, page_size=spec.page_size, num_pages=spec.num_pages,
+                   softmax_scale=spec.softmax_scale, prefix_lens=spec.prefix_lens, chunk_lens=spec.chunk_lens,
+                   block_table=spec.block_table, kv_shared=spec.kv_shared, max_splits=max_splits)
+
+
+def _q4_shapes(p: Plan) -> dict:
+    sh = _attn_shapes(p)
+    if "pool" not in sh:
+        raise ValueError("the plan is of a bf16 cache: make it with q4_plan")
+    return sh
+
+
+def _required(**bufs):
+    for name, t in bufs.items():
+        if t is None:
+            raise ValueError(f"{name} is required")
+
+
+def q4_append_kv(p: Plan, k_new, v_new, k_pool, v_pool, workspace, stream=None):
+    """Quantise the wave's new K/V rows into their pages."""
+    import torch
+    bf, _ = _dtypes()
+    sh = _q4_shapes(p)
+    _required(k_new=k_new, v_new=v_new, k_pool=k_pool, v_pool=v_pool)
+    _check_shapes(("k_new", k_new, sh["k_new"]), ("v_new", v_new, sh["v_new"]), ("k_pool", k_pool, sh["pool"]),
+                  ("v_pool", v_pool, sh["pool"]))
+    _check(load_library().wavepp_q4_append_kv(
+        p.handle, _ptr(k_new, bf, "k_new"), _ptr(v_new, bf, "v_new"), _ptr(k_pool, torch.uint8, "k_pool"),
+        _ptr(v_pool, torch.uint8, "v_pool"), _ptr(workspace, name="workspace"), workspace.nbytes, _stream_for(stream, k_new, v_new, k_pool, v_pool, workspace)))
+
+
+def q4_read_kv(p: Plan, k_pool, v_pool, k_out, v_out, workspace, stream=None):
+    """The bf16 rows of the wave's new tokens as the pages hold them."""
+    import torch
+    bf, _ = _dtypes()
+    sh = _q4_shapes(p)
+    _required(k_pool=k_pool, v_pool=v_pool, k_out=k_out, v_out=v_out)
+    _check_shapes(("k_pool", k_pool, sh["pool"]), ("v_pool", v_pool, sh["pool"]), ("k_out", k_out, sh["k_new"]),
+                  ("v_out", v_out, sh["v_new"]))
+    _check(load_library().wavepp_q4_read_kv(
+        p.handle, _ptr(k_pool, torch.uint8, "k_pool"), _ptr(v_pool, torch.uint8, "v_pool"), _ptr(k_out, bf, "k_out"),
+        _ptr(v_out, bf, "v_out"), _ptr(workspace, name="workspace"), workspace.nbytes, _stream_for(stream, k_pool, v_pool, k_out, v_out, workspace)))
+
+
+def q4_chunked_prefill(p: Plan, q, k_pool, v_pool, out, lse, workspace, stream=None):
+    """Attention of the wave's queries over 4-bit pages (lse may be None)."""
+    import torch
+    bf, f32 = _dtypes()
+    sh = _q4_shapes(p)
+    _required(q=q, k_pool=k_pool, v_pool=v_pool, out=out)
+    _check_shapes(("q", q, sh["q"]), ("k_pool", k_pool, sh["pool"]), ("v_pool", v_pool, sh["pool"]),
+                  ("out", out, sh["out"]), ("lse", lse, sh["lse"]))
+    _check(load_library().wavepp_q4_chunked_prefill(
+        p.handle, _ptr(q, bf, "q"), _ptr(k_pool, torch.uint8, "k_pool"), _ptr(v_pool, torch.uint8, "v_pool"),
+        _ptr(out, bf, "out"), _ptr(lse, f32, "lse"), _ptr(workspace, name="workspace"), workspace.nbytes,
+        _stream_for(stream, q, k_pool, v_pool, out, lse, workspace)))
 
 
 # ------------------------------------------------------------------------------------------------

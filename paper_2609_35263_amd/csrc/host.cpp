@@ -7,6 +7,7 @@
 // that does not match the materialized cache must fail rather than run).
 #include "wavepp_attn.h"
 #include "internal.h"
+#include "plan.h"
 
 #include <hip/hip_runtime.h>
 
@@ -18,35 +19,15 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <numeric>
 #include <string>
 #include <unordered_map>
 #include <vector>
 
 using namespace wavepp;
-
-struct wavepp_plan {
-  wavepp_attn_shape shape;
-  int32_t num_requests = 0;
-  int32_t bt_stride = 0;
-  int64_t total_tokens = 0;
-  uint32_t serial = 0;
-  int32_t rows_per_item = 0;
-  int32_t kv_tile = 0;
-  int32_t max_splits_used = 1;
-  int32_t num_real_items = 0;
-  std::vector<WorkItem> items;
-  std::vector<MergeItem> merges;      // those that merge_wide_kernel takes first
-  int32_t num_merge_wide = 0, merge_rows = 0;
-  int64_t partial_rows = 0;
-  // metadata blob (uploaded as is) and its sub-array offsets
-  std::vector<unsigned char> blob;
-  size_t off_reqs = 0, off_bt = 0, off_items = 0, off_merges = 0;
-  size_t meta_bytes = 0;       // blob size rounded up to 256
-  size_t off_opart = 0, off_lpart = 0;
-  size_t workspace_bytes = 0;
-};
 
 namespace wavepp {
 namespace {
@@ -612,7 +593,7 @@ int stage_and_copy(const void* src, size_t bytes, void* dst, hipStream_t stream)
 
 }  // namespace wavepp
 
-namespace {
+namespace wavepp {
 
 int check_workspace(const wavepp_plan* plan, void* ws, size_t ws_bytes) {
   if (!ws) return set_error(WAVEPP_EINVAL, "workspace is NULL");
@@ -622,7 +603,11 @@ int check_workspace(const wavepp_plan* plan, void* ws, size_t ws_bytes) {
   return WAVEPP_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int require_cache(const wavepp_plan* plan, bool q4) {
+  if (plan->q4 == q4) return WAVEPP_OK;
+  return plan->q4 ? set_error(WAVEPP_EINVAL, "the plan is of a 4-bit cache: use the wavepp_q4 entry points")
+                  : set_error(WAVEPP_EINVAL, "the plan is of a bf16 cache: make it with wavepp_q4_plan");
+}
 
 DevPlan make_dev(const wavepp_plan* plan, void* ws) {
   auto* base = static_cast<unsigned char*>(ws);
@@ -652,28 +637,8 @@ DevPlan make_dev(const wavepp_plan* plan, void* ws) {
   return d;
 }
 
-}  // namespace
-
-extern "C" {
-
-const char* wavepp_status_string(int status) {
-  switch (status) {
-    case WAVEPP_OK: return "WAVEPP_OK";
-    case WAVEPP_EINVAL: return "WAVEPP_EINVAL: invalid argument";
-    case WAVEPP_EUNSUPPORTED: return "WAVEPP_EUNSUPPORTED: unsupported shape";
-    case WAVEPP_ERANGE: return "WAVEPP_ERANGE: block-table entry outside the page pool";
-    case WAVEPP_EALIAS: return "WAVEPP_EALIAS: appended page also referenced elsewhere";
-    case WAVEPP_EPOSITION: return "WAVEPP_EPOSITION: span not backed by the block table";
-    case WAVEPP_ENOSPACE: return "WAVEPP_ENOSPACE: workspace too small";
-    case WAVEPP_EHIP: return "WAVEPP_EHIP: HIP runtime error";
-    default: return "unknown wavepp status";
-  }
-}
-
-const char* wavepp_last_error(void) { return last_error_text(); }
-
-int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits,
-                     wavepp_plan** out) {
+int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, bool q4,
+              wavepp_plan** out) {
   clear_error();
   if (!shape || !batch || !out) return set_error(WAVEPP_EINVAL, "null argument");
   *out = nullptr;
@@ -687,9 +652,10 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
     return set_error(WAVEPP_EINVAL, "num_q_heads (%d) is not a multiple of num_kv_heads (%d)", s.num_q_heads,
                 s.num_kv_heads);
   if (s.kv_shared != 0 && s.kv_shared != 1) return set_error(WAVEPP_EINVAL, "kv_shared must be 0 or 1");
-  if (!supported_shape(s))
-    return set_error(WAVEPP_EUNSUPPORTED, "unsupported (head_dim_qk=%d, head_dim_v=%d, page_size=%d, kv_shared=%d, "
-                "num_kv_heads=%d)", s.head_dim_qk, s.head_dim_v, s.page_size, s.kv_shared, s.num_kv_heads);
+  if (!supported_shape(s) || (q4 && s.kv_shared))
+    return set_error(WAVEPP_EUNSUPPORTED, "unsupported%s (head_dim_qk=%d, head_dim_v=%d, page_size=%d, kv_shared=%d, "
+                "num_kv_heads=%d)", q4 ? " for a 4-bit cache" : "", s.head_dim_qk, s.head_dim_v, s.page_size, s.kv_shared,
+                s.num_kv_heads);
   if (max_splits < 0) return set_error(WAVEPP_EINVAL, "max_splits must be >= 0");
   const int32_t R = batch->num_requests;
   if (R < 0) return set_error(WAVEPP_EINVAL, "num_requests < 0");
@@ -731,9 +697,10 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
                     "times in the wave", r, (long long)b, row[b], refcount[row[b]]);
   }
 
-  auto plan = new (std::nothrow) wavepp_plan();
+  std::unique_ptr<wavepp_plan> plan(new (std::nothrow) wavepp_plan());
   if (!plan) return set_error(WAVEPP_EINVAL, "out of host memory");
   plan->shape = s;
+  plan->q4 = q4;
   plan->num_requests = R;
   plan->bt_stride = stride;
   plan->total_tokens = total;
@@ -749,11 +716,14 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
   const char* gw = getenv("WAVEPP_GQA_WAVES");
   const int gw_n = gw ? atoi(gw) : 0;
   const bool small_rows = gw_n == 4 || (gw_n != 8 && max_rows <= kGqaRowsPerItem / 2);
-  const int gqa_rows = small_rows ? kGqaRowsPerItem / 2 : kGqaRowsPerItem;
+  // Over 4-bit pages, up to 32 rows for every (request, KV head) -- a token or a few -- run with one wave's rows and
+  // the keys of a tile shared out over the four waves of a workgroup.
+  const bool few_rows = q4 && gw_n == 0 && max_rows <= kQ4FewRows;
+  const int gqa_rows = few_rows ? kQ4FewRows : small_rows ? kGqaRowsPerItem / 2 : kGqaRowsPerItem;
   const int M = mla ? kMlaRowsPerItem : gqa_rows;
   // keys per tile of the kernel that will run the plan (the 4-wave grouped form uses half tiles);
   // split boundaries fall on whole tiles of it
-  const int KT = mla ? kMlaKvTile : (small_rows ? kKvTile / 2 : kKvTile);
+  const int KT = mla ? kMlaKvTile : few_rows ? kQ4FewTile : (small_rows ? kKvTile / 2 : kKvTile);
   plan->rows_per_item = M;
   plan->kv_tile = KT;
 
@@ -792,7 +762,7 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
   // row tile) the same number of splits: such a wave runs as one round of workgroups and lasts as
   // long as its longest item, so requests with longer prefixes take more splits.
   const int64_t fill_target = 512;
-  const int64_t min_split_tiles = (mla ? 512 : 1024) / KT;
+  const int64_t min_split_tiles = (mla ? 512 : few_rows ? 256 : 1024) / KT;
   std::vector<int64_t> ntiles(base.size());
   for (size_t i = 0; i < base.size(); ++i) ntiles[i] = ceil_div(base[i].kv_end, KT);
   SplitPlan split{ntiles, int64_t(base.size())};
@@ -910,10 +880,7 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
       items.push_back(x);
     }
     part_rows += S * w.rows;
-    if (part_rows > INT32_MAX / 2) {
-      delete plan;
-      return set_error(WAVEPP_EINVAL, "split partials too large");
-    }
+    if (part_rows > INT32_MAX / 2) return set_error(WAVEPP_EINVAL, "split partials too large");
   }
   plan->num_real_items = int32_t(items.size());
   plan->max_splits_used = max_used;
@@ -924,10 +891,7 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
   const int per_cu = small_rows && !mla ? (s.head_dim_qk == 64 ? 3 : 2) : 1;
   plan->items = order_items(std::move(items), G, env_flag("WAVEPP_XCD_ORDER", true),
                             env_flag("WAVEPP_STREAM_MAJOR", true), per_cu * kNumCu, KT, mla ? 5.0 : 1.0, mla || small_rows ? 1.0 : kModel128.idle);
-  if (plan->items.size() > size_t(INT32_MAX / 2)) {
-    delete plan;
-    return set_error(WAVEPP_EINVAL, "too many work items");
-  }
+  if (plan->items.size() > size_t(INT32_MAX / 2)) return set_error(WAVEPP_EINVAL, "too many work items");
 
   // --- metadata blob -------------------------------------------------------------------------------
   size_t off = align_up(sizeof(MetaHeader), 16);
@@ -960,8 +924,39 @@ int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, 
   plan->off_opart = plan->meta_bytes;
   plan->off_lpart = align_up(plan->off_opart + sizeof(float) * size_t(part_rows) * size_t(s.head_dim_v), 256);
   plan->workspace_bytes = align_up(plan->off_lpart + sizeof(float) * size_t(part_rows), 256);
-  *out = plan;
+  *out = plan.release();
   return WAVEPP_OK;
+}
+
+}  // namespace wavepp
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace
+
+extern "C" {
+
+const char* wavepp_status_string(int status) {
+  switch (status) {
+    case WAVEPP_OK: return "WAVEPP_OK";
+    case WAVEPP_EINVAL: return "WAVEPP_EINVAL: invalid argument";
+    case WAVEPP_EUNSUPPORTED: return "WAVEPP_EUNSUPPORTED: unsupported shape";
+    case WAVEPP_ERANGE: return "WAVEPP_ERANGE: block-table entry outside the page pool";
+    case WAVEPP_EALIAS: return "WAVEPP_EALIAS: appended page also referenced elsewhere";
+    case WAVEPP_EPOSITION: return "WAVEPP_EPOSITION: span not backed by the block table";
+    case WAVEPP_ENOSPACE: return "WAVEPP_ENOSPACE: workspace too small";
+    case WAVEPP_EHIP: return "WAVEPP_EHIP: HIP runtime error";
+    default: return "unknown wavepp status";
+  }
+}
+
+const char* wavepp_last_error(void) { return last_error_text(); }
+
+int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits,
+                     wavepp_plan** out) {
+  return plan_wave(shape, batch, max_splits, false, out);
 }
 
 size_t wavepp_plan_workspace_bytes(const wavepp_plan* plan) { return plan ? plan->workspace_bytes : 0; }
@@ -1007,7 +1002,8 @@ int wavepp_attn_append_kv(const wavepp_plan* plan, const void* k_new, const void
                           void* workspace, size_t ws_bytes, hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  int st = check_workspace(plan, workspace, ws_bytes);
+  int st = require_cache(plan, false);
+  if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st) return st;
   const bool shared = plan->shape.kv_shared != 0;
   if (plan->total_tokens == 0) return WAVEPP_OK;
@@ -1028,7 +1024,8 @@ int wavepp_attn_chunked_prefill(const wavepp_plan* plan, const void* q, const vo
                                 void* out, float* lse, void* workspace, size_t ws_bytes, hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  int st = check_workspace(plan, workspace, ws_bytes);
+  int st = require_cache(plan, false);
+  if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st) return st;
   const bool shared = plan->shape.kv_shared != 0;
   if (plan->total_tokens == 0) return WAVEPP_OK;
@@ -1055,6 +1052,7 @@ int wavepp_attn_chunked_prefill_noalloc(const wavepp_plan* plan, const void* q, 
                                         hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
+  if (int st = require_cache(plan, false)) return st;
   if (plan->workspace_bytes > kNoAllocScratchBytes)
     return set_error(WAVEPP_ENOSPACE, "plan needs %zu bytes of scratch, the static scratch holds %zu: plan the wave "
                      "with fewer key-range splits (max_splits) or call wavepp_attn_chunked_prefill with a workspace",

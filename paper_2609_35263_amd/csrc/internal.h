@@ -15,6 +15,9 @@ constexpr int kNumXcd = 8;                 // L2 domains a launch is spread over
 constexpr int kNumEngines = 32;            // shader engines, which workgroups go to in turn
 constexpr int kMlaRowsPerItem = 128;       // latent kernel: query rows per work item
 constexpr int kMlaKvTile = 64;             // latent kernel: keys per tile
+constexpr int kQ4FewRows = 32;             // 4-bit pages, few rows: query rows per work item (every wave has them all)
+constexpr int kQ4FewTile = 128;            // 4-bit pages, few rows: keys per step of a workgroup, 32 a wave
+constexpr int kQ4Block = 32;               // values along the head dim that share a scale
 constexpr int kMergeNarrow = 16;           // merge: splits whose partials one thread loads at once
 
 // Header at the start of the uploaded metadata.
@@ -141,6 +144,13 @@ hipError_t launch_append(const DevPlan& p, const void* k_new, const void* v_new,
                          hipStream_t stream);
 hipError_t launch_attention(const DevPlan& p, const void* q, const void* k_pool, const void* v_pool, void* out,
                             float* lse, hipStream_t stream);
+// The same over 4-bit pages, and the way back from them to bf16 rows.
+hipError_t launch_q4_append(const DevPlan& p, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
+                            hipStream_t stream);
+hipError_t launch_q4_read(const DevPlan& p, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
+                          hipStream_t stream);
+hipError_t launch_q4_attention(const DevPlan& p, const void* q, const void* k_pool, const void* v_pool, void* out,
+                               float* lse, hipStream_t stream);
 hipError_t launch_merge(const DevPlan& p, void* out, float* lse, hipStream_t stream);
 // Copy `bytes` (a multiple of 16, both pointers 16-byte aligned) from device-visible pinned host
 // memory to device memory with a kernel on `stream`.

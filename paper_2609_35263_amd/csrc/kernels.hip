@@ -25,6 +25,7 @@
 //     the output.
 #include <hip/hip_runtime.h>
 
+#include "device.h"
 #include "internal.h"
 
 #include <algorithm>
@@ -32,23 +33,6 @@
 #include <type_traits>
 
 namespace wavepp {
-
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ bool meta_ok(const DevPlan& p) {
-  return p.hdr->magic == kMagic && p.hdr->serial == p.serial;
-}
-
-__device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // ---------------------------------------------------------------------------------------------
 // Append: token t of request r -> page bt[r][(p_r + i) / B], slot (p_r + i) % B, all KV heads.
@@ -68,11 +52,6 @@ __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_ex
 // 14.2 / 13.4; 16 heads, two chunks a thread: 4,104 tokens 33.4 / 23.4.  From warm memory 8,192 tokens of 8 heads
 // take 14.8 / 12.7 us, 65,536 latent rows 33.2 / 27.4.
 // ---------------------------------------------------------------------------------------------
-template <typename T>
-__device__ __forceinline__ T const_load(const T* ptr) {
-  return *((const __attribute__((address_space(4))) T*)(ptr));
-}
-
 template <int DK, int DV, int TOK, bool EARLY>
 __global__ __launch_bounds__(256) void append_kernel(DevPlan p, const uint4* __restrict__ k_new,
                                                      const uint4* __restrict__ v_new, uint4* __restrict__ k_pool,
@@ -137,27 +116,6 @@ __global__ __launch_bounds__(256) void append_kernel(DevPlan p, const uint4* __r
 // ---------------------------------------------------------------------------------------------
 // Grouped-query attention, head dim D (64 or 128), page size PAGE (16 or 64).
 // ---------------------------------------------------------------------------------------------
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
-// Both halves of the wave receive max / sum of their value and the other half's value for the
-// same query row (lanes l and l ^ 32).
-__device__ __forceinline__ float halves_max(float x) {
-  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
-}
-__device__ __forceinline__ float halves_sum(float x) {
-  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
-}
-
-// Transposing LDS read: within each group of 16 lanes, lane i receives element i%4 of the 8 bytes
-// addressed by lanes 4m + i/4, m = 0..3.
-__device__ __forceinline__ bf16x4 lds_read_tr(const __bf16* p) {
-  const i16x4 r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p));
-  return __builtin_bit_cast(bf16x4, r);
-}
-
 template <int D, int PAGE, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_gqa_kernel(DevPlan p, const __bf16* __restrict__ q,
                                                           const __bf16* __restrict__ kpool,

@@ -1,0 +1,315 @@
+"""The 4-bit paged cache on the GPU against its fp64 oracle, through the C ABI.
+
+Tolerances, fixed before the first run.  Append and read: exact, bytes and bits.  Attention: the operands are the cached
+values exactly, and what is rounded to bf16 is every probability (half a step, 2^-8 of itself) and the
+output (2^-8 of itself).  So an output is off by at most 2^-8 sum p|v| + 2^-8 |o| <= 2^-7 sum p|v|, and the fp32 sums,
+exponentials and logits (errors near 1e-5 of a probability) stay far inside the tenth that is added.
+LSE: a logit is a sum of 128 products in fp32, off by at most 128 * 2^-24 * sum |q k| scale; with these inputs the sums
+stay under 12, which gives 9e-5: 1e-4.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_35263_amd as wp
+import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+MERGED = 1.1 * 2.0 ** -7
+LSE = 1e-4
+
+
+def make(spec, seed, garbage=True):
+    """q, k_new, v_new and pools whose cached slots hold rounded N(0, 1) rows; every other slot holds any bytes."""
+    rng, any_bytes = np.random.default_rng(seed), np.random.default_rng(seed + 1000)
+    t = wl.make_tensors(spec, seed, poison=False)
+    P, H, B, d = spec.num_pages, spec.num_kv_heads, spec.page_size, spec.head_dim_qk
+    t = {n: t[n] for n in ("q", "k_new", "v_new")}
+    cnt = wl.prefix_slot_counts(spec)
+    used = np.arange(B)[None, :] < cnt[:, None]
+    for name in ("k_pool", "v_pool"):
+        x = torch.as_tensor(rng.standard_normal((P, H, B, d)).astype(np.float32)).to(torch.bfloat16)
+        codes, scales = oracle.q4.quantise(wl.to_bits(x))
+        if garbage:
+            gap = ~used[:, None, :, None]
+            codes = np.where(gap, any_bytes.integers(0, 16, codes.shape), codes).astype(np.uint8)
+            scales = np.where(gap, any_bytes.integers(0, 256, scales.shape), scales).astype(np.uint8)
+        t[name] = torch.from_numpy(oracle.q4.join_pool(codes, scales))
+    return t
+
+
+def same(a, b):
+    """Whether two tensors hold the same bits."""
+    return bool(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)))
+
+
+def on_gpu(spec, t, max_splits=0, append=True, plan=None):
+    d = {n: x.cuda() for n, x in t.items()}
+    p = plan or wp.q4_plan_for(spec, max_splits=max_splits)
+    ws = wp.new_workspace(p)
+    out = torch.full((spec.total_tokens, spec.num_q_heads, spec.head_dim_v), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((spec.total_tokens, spec.num_q_heads), float("nan"), device="cuda")
+    wp.plan_upload(p, ws)
+    if append:
+        wp.q4_append_kv(p, d["k_new"], d["v_new"], d["k_pool"], d["v_pool"], ws)
+    wp.q4_chunked_prefill(p, d["q"], d["k_pool"], d["v_pool"], out, lse, ws)
+    torch.cuda.synchronize()
+    return {**d, "out": out, "lse": lse, "plan": p, "ws": ws}
+
+
+def appended(spec, t):
+    d, B = spec.head_dim_qk, spec.page_size
+    return [oracle.q4.append(t[f"{n}_pool"].numpy(), wl.to_bits(t[f"{n}_new"]), spec.prefix_lens, spec.chunk_lens,
+                             spec.block_table, d, B) for n in "kv"]
+
+
+def check(spec, t, g, what=""):
+    d, B = spec.head_dim_qk, spec.page_size
+    k, v = appended(spec, t)
+    assert np.array_equal(g["k_pool"].cpu().numpy(), k) and np.array_equal(g["v_pool"].cpu().numpy(), v), "pool bytes"
+    with np.errstate(over="ignore", invalid="ignore"):
+        o, lse, size = oracle.q4.attention(wl.to_bits(t["q"]), oracle.q4.pool_values(k, d, B), oracle.q4.pool_values(v, d, B),
+                                           spec.prefix_lens, spec.chunk_lens, spec.block_table, B, spec.softmax_scale)
+    err = np.abs(g["out"].float().cpu().numpy().astype(np.float64) - o)
+    lerr = np.abs(g["lse"].cpu().numpy().astype(np.float64) - lse)
+    print(f"[q4] {spec.name} {what}: out {(err / np.maximum(size, 1e-300)).max() / MERGED:.2f} of its bound, lse {lerr.max():.1e}", flush=True)
+    assert (err <= MERGED * size).all() and (lerr <= LSE).all()
+
+
+def test_rounding_of_every_bf16_number():
+    """Every bf16 bit pattern, infinities and NaN among them, next to a block maximum of its own size, of 7 / 4 and of 3 times
+    it, and of 1: codes, scale bytes and the values read back."""
+    every = np.arange(1 << 16, dtype=np.uint32).astype(np.uint16)
+    with np.errstate(over="ignore", invalid="ignore"):
+        x = oracle.bf16_bits_to_f64(every)
+        tops = [np.abs(x), np.abs(x) * 1.75, np.abs(x) * 3.0, np.ones_like(x), np.full_like(x, 2.0 ** -110)]
+    rows = []
+    for top in tops:
+        top = torch.as_tensor(np.nan_to_num(top, nan=1.0, posinf=3e38).clip(0, 3.3e38)).to(torch.bfloat16)
+        r = np.zeros((1 << 16, 32), dtype=np.uint16)
+        r[:, 0], r[:, 17] = every, wl.to_bits(top)
+        rows.append(r.reshape(-1, 128))
+    rows = np.concatenate(rows)
+    n = 2 * ((rows.shape[0] + 1) // 2)
+    rows = np.concatenate((rows, np.zeros((n - rows.shape[0], 128), dtype=np.uint16))).reshape(-1, 2, 128)
+    T = rows.shape[0]
+    spec = wl.custom_wave(2, 2, 128, 128, 64, [0], [T], seed=1, name="rounding")
+    p = wp.q4_plan_for(spec)
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    new = torch.from_numpy(rows.view(np.int16)).view(torch.bfloat16).cuda()
+    flipped = new.flip(0).contiguous()
+    pools = [wp.q4_new_pool(spec.num_pages, 2, 128, 64) for _ in range(2)]
+    back = [torch.empty_like(new) for _ in range(2)]
+    wp.q4_append_kv(p, new, flipped, *pools, ws)
+    wp.q4_read_kv(p, *pools, *back, ws)
+    torch.cuda.synchronize()
+    codes, scales = oracle.q4.quantise(rows)
+    for pool, order in zip(pools, (slice(None), slice(None, None, -1))):
+        c, s = oracle.q4.split_pool(pool.cpu().numpy(), 128, 64)
+        pages = spec.block_table[0][np.arange(T) // 64]
+        assert np.array_equal(s[pages, :, np.arange(T) % 64], scales[order])
+        assert np.array_equal(c[pages, :, np.arange(T) % 64], codes[order])
+    want = oracle.q4.values(codes, scales)
+    assert np.array_equal(back[0].double().cpu().numpy(), want)
+    assert np.array_equal(back[1].double().cpu().numpy(), want[::-1])
+
+
+def test_every_code_with_every_scale():
+    """The values that the read gives for all 16 codes under the 245 scale bytes that the append writes."""
+    rng = np.random.default_rng(2)
+    T = 245
+    codes = rng.integers(0, 16, (T, 1, 64)).astype(np.uint8)
+    codes[:, 0, :16] = np.arange(16)
+    scales = np.stack((np.arange(8, 253), np.arange(8, 253)[::-1]), axis=-1).astype(np.uint8)[:, None]
+    spec = wl.custom_wave(1, 1, 64, 64, 16, [0], [T], seed=2, name="codes")
+    c, s = np.zeros((spec.num_pages, 1, 16, 64), np.uint8), np.zeros((spec.num_pages, 1, 16, 2), np.uint8)
+    pages, slots = spec.block_table[0][np.arange(T) // 16], np.arange(T) % 16
+    c[pages, :, slots], s[pages, :, slots] = codes, scales
+    pool = torch.from_numpy(oracle.q4.join_pool(c, s)).cuda()
+    p = wp.q4_plan_for(spec)
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    out = [torch.empty(T, 1, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    wp.q4_read_kv(p, pool, pool, *out, ws)
+    want = oracle.q4.values(codes, scales)
+    for x in out:
+        assert np.array_equal(x.double().cpu().numpy(), want)
+        assert np.array_equal(np.signbit(x.float().cpu().numpy()), codes >= 8)
+
+
+WAVES = {
+    # name: (q heads, KV heads, dim, page, prefix, chunk)
+    "one_token": (8, 2, 64, 16, [0], [1]),
+    "first_tokens": (32, 8, 128, 64, [0, 0, 1, 31, 32, 33], [1, 2, 1, 1, 1, 1]),
+    "tokens": (64, 8, 128, 64, [700, 63, 64, 1, 500, 0], [1, 1, 1, 1, 0, 1]),
+    "tokens_small": (24, 4, 64, 16, [300, 15, 16, 129, 0], [1, 1, 1, 1, 1]),
+    "tokens_no_groups": (4, 4, 128, 16, [255, 300, 16], [1, 1, 3]),
+    "few_rows_full": (32, 1, 64, 64, [90, 400], [1, 1]),
+    "few_rows_mixed": (16, 2, 128, 64, [200, 31, 333], [4, 2, 3]),
+    "four_waves": (16, 2, 128, 64, [100, 0, 77], [9, 16, 1]),
+    "four_waves_small": (24, 4, 64, 16, [50, 3], [17, 21]),
+    "wide_group": (16, 1, 128, 64, [130], [7]),
+    "eight_waves": (8, 2, 128, 64, [70, 0, 0], [150, 40, 65]),
+    "eight_waves_small": (8, 2, 64, 16, [33, 5], [130, 70]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(WAVES))
+@pytest.mark.parametrize("splits", [0, 1, 3])
+def test_attention_against_the_oracle(name, splits):
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=11, name=name)
+    t = make(spec, 12)
+    check(spec, t, on_gpu(spec, t, max_splits=splits), f"splits {splits}")
+
+
+@pytest.mark.parametrize("q,kv,dim,page", [(64, 8, 128, 64), (24, 4, 64, 16)])
+def test_long_cache_and_many_splits(q, kv, dim, page):
+    spec = wl.custom_wave(q, kv, dim, dim, page, [9000, 2049], [1, 1], seed=13, name=f"long_{dim}")
+    t = make(spec, 14)
+    g = on_gpu(spec, t)
+    assert g["plan"].info()["max_splits"] > 4
+    check(spec, t, g)
+
+
+def test_large_logits_and_a_needle():
+    """Keys that dominate, first and last: the running maximum moves by far more than its slack, and back."""
+    spec = wl.custom_wave(16, 2, 128, 128, 64, [300, 400], [1, 30], seed=15, name="needle")
+    for scale in (30.0, 1e-3):
+        t = make(spec, 16)
+        t["q"] = (t["q"].float() * scale).to(torch.bfloat16)
+        g = on_gpu(spec, t)
+        k, v = appended(spec, t)
+        o, lse, size = oracle.q4.attention(wl.to_bits(t["q"]), oracle.q4.pool_values(k, 128, 64), oracle.q4.pool_values(v, 128, 64),
+                                           spec.prefix_lens, spec.chunk_lens, spec.block_table, 64, spec.softmax_scale)
+        err = np.abs(g["out"].float().cpu().numpy() - o)
+        # logits are `scale` times larger, and so is what fp32 loses of them: 9e-5 scale of a probability
+        assert (err <= (MERGED + 2e-4 * scale) * size).all()
+        assert (np.abs(g["lse"].cpu().numpy() - lse) <= LSE * max(1.0, scale)).all()
+
+
+def test_stale_slots_and_later_tokens_do_not_leak():
+    """Bytes behind the last token, and what a later token of the chunk holds (NaN, infinities), leave a row as it is."""
+    for name in ("few_rows_mixed", "four_waves", "eight_waves"):
+        q, kv, dim, page, prefix, chunk = WAVES[name]
+        spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=17, name=name)
+        t = make(spec, 18)
+        a = on_gpu(spec, t)
+        other = make(spec, 18, garbage=False)
+        b = on_gpu(spec, {**t, **{n: other[n] for n in ("k_pool", "v_pool")}})
+        assert same(a["out"], b["out"])
+        assert same(a["lse"], b["lse"])
+        ends = np.cumsum(spec.chunk_lens) - 1
+        bad = {n: x.clone() for n, x in t.items()}
+        bad["k_new"][ends[0]], bad["v_new"][ends[0]] = float("nan"), float("inf")
+        c = on_gpu(spec, bad)
+        keep = np.arange(spec.total_tokens) != ends[0]
+        assert same(a["out"][keep], c["out"][keep])
+        seen = c["out"][ends[0]].float()
+        assert not (seen.abs() < 1e30).any(), "a row that sees the bad token shows it"
+
+
+def test_repeated_calls_and_page_orders_are_bit_identical():
+    spec = wl.custom_wave(64, 8, 128, 128, 64, [1500, 700, 64], [1, 1, 1], seed=19, name="repeat")
+    t = make(spec, 20)
+    a, b = on_gpu(spec, t), on_gpu(spec, t)
+    assert a["plan"].info()["max_splits"] > 1
+    assert same(a["out"], b["out"])
+    perm = np.random.default_rng(21).permutation(spec.num_pages).astype(np.int32)
+    moved = {**t, **{n: torch.empty_like(t[n]) for n in ("k_pool", "v_pool")}}
+    for n in ("k_pool", "v_pool"):
+        moved[n][perm] = t[n]
+    other = wl.custom_wave(64, 8, 128, 128, 64, [1500, 700, 64], [1, 1, 1], seed=19, name="repeat")
+    other.block_table = np.where(other.block_table >= 0, perm[np.maximum(other.block_table, 0)], -1).astype(np.int32)
+    c = on_gpu(other, moved)
+    assert same(a["out"], c["out"])
+    assert same(a["lse"], c["lse"])
+
+
+def test_shared_prefix_pages():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [64, 64, 64], [1, 2, 1], seed=22, shared_prefix_pages=3, name="shared")
+    t = make(spec, 23)
+    check(spec, t, on_gpu(spec, t))
+
+
+def test_graph_replays_and_streams_match_eager():
+    """Append and attention captured once and replayed with new inputs in the same buffers, eager work in between."""
+    spec = wl.custom_wave(64, 8, 128, 128, 64, [3000, 130, 5], [1, 1, 1], seed=24, name="graph")
+    t = [make(spec, 25 + i) for i in range(3)]
+    eager = [on_gpu(spec, x) for x in t]
+    p = eager[0]["plan"]
+    assert p.info()["num_merge_items"] > 0
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    buf = {n: x.cuda() for n, x in t[0].items()}
+    out, lse = torch.empty_like(eager[0]["out"]), torch.empty_like(eager[0]["lse"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        wp.q4_append_kv(p, buf["k_new"], buf["v_new"], buf["k_pool"], buf["v_pool"], ws)
+        wp.q4_chunked_prefill(p, buf["q"], buf["k_pool"], buf["v_pool"], out, lse, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert same(out, eager[0]["out"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        wp.q4_append_kv(p, buf["k_new"], buf["v_new"], buf["k_pool"], buf["v_pool"], ws)
+        wp.q4_chunked_prefill(p, buf["q"], buf["k_pool"], buf["v_pool"], out, lse, ws)
+    for i in (0, 1, 2, 1):
+        for n, x in t[i].items():
+            buf[n].copy_(x)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("out", "lse", "k_pool", "v_pool"):
+            got = {"out": out, "lse": lse, **buf}[n]
+            assert same(got, eager[i][n]), (i, n)
+
+
+def test_two_plans_on_two_streams():
+    specs = [wl.custom_wave(64, 8, 128, 128, 64, [2500 + 100 * i, 40], [1, 2], seed=30 + i, name=f"stream{i}") for i in range(2)]
+    t = [make(s, 32 + i) for i, s in enumerate(specs)]
+    want = [on_gpu(s, x) for s, x in zip(specs, t)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got.clear()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                w = want[i]
+                out, lse = torch.empty_like(w["out"]), torch.empty_like(w["lse"])
+                wp.q4_chunked_prefill(w["plan"], w["q"], w["k_pool"], w["v_pool"], out, lse, w["ws"])
+                got.append(out)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert same(got[i], want[i]["out"])
+
+
+def test_lse_is_optional_and_idle_waves_do_nothing():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [1, 3], seed=26, name="no_lse")
+    t = make(spec, 27)
+    g = on_gpu(spec, t)
+    out = torch.empty_like(g["out"])
+    wp.q4_chunked_prefill(g["plan"], g["q"], g["k_pool"], g["v_pool"], out, None, g["ws"])
+    assert same(out, g["out"])
+    idle = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [0, 0], seed=28, name="idle")
+    t = make(idle, 29)
+    g = on_gpu(idle, t)
+    assert g["out"].shape[0] == 0 and torch.equal(g["k_pool"].cpu(), t["k_pool"])
+
+
+def test_a_workspace_overwritten_since_its_upload_writes_nothing():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [1, 3], seed=26, name="stale")
+    t = make(spec, 27)
+    g = on_gpu(spec, t)
+    ws = torch.zeros_like(g["ws"])
+    wp.plan_upload(g["plan"], ws)
+    ws.zero_()
+    out, before = torch.zeros_like(g["out"]), g["k_pool"].clone()
+    wp.q4_append_kv(g["plan"], g["v_new"], g["k_new"], g["k_pool"], g["v_pool"], ws)
+    wp.q4_chunked_prefill(g["plan"], g["q"], g["k_pool"], g["v_pool"], out, None, ws)
+    assert not out.view(torch.int16).any() and torch.equal(before, g["k_pool"])
