@@ -20,4 +20,4 @@ from .attention import (  # noqa: F401
     probabilities,
     merge_partials,
 )
-from . import kda, q4  # noqa: F401,E402
+from . import kda, lin, q4  # noqa: F401,E402

@@ -26,6 +26,12 @@ Per wave of a KDA layer:
     ws = new_workspace(kp)
     kda_upload(kp, ws)
     kda_chunked_prefill(kp, q, k, v, alpha, beta, state_pool, out, ws)
+
+Per wave of a linear-attention layer, single tokens included (their plan serves every step of the batch):
+    lp = lin_plan(...)                  # host: validate chunk lengths and snapshot slots
+    ws = new_workspace(lp)
+    lin_upload(lp, ws)
+    lin_chunked_prefill(lp, q, k, v, alpha, state_pool, out, ws)
 """
 import ctypes
 import os
@@ -47,7 +53,11 @@ EXPORTED_SYMBOLS = [
 Q4_SYMBOLS = [
     "wavepp_q4_page_bytes", "wavepp_q4_plan", "wavepp_q4_append_kv", "wavepp_q4_read_kv", "wavepp_q4_chunked_prefill",
 ]
-EXPORTED_SYMBOLS += Q4_SYMBOLS
+LIN_SYMBOLS = [
+    "wavepp_lin_plan", "wavepp_lin_workspace_bytes", "wavepp_lin_get_info", "wavepp_lin_upload",
+    "wavepp_lin_chunked_prefill", "wavepp_lin_destroy",
+]
+EXPORTED_SYMBOLS += Q4_SYMBOLS + LIN_SYMBOLS
 MPU_SYMBOLS = [
     "wavepp_mpu_budget_ladder", "wavepp_mpu_create", "wavepp_mpu_admit", "wavepp_mpu_plan", "wavepp_mpu_commit",
     "wavepp_mpu_retire", "wavepp_mpu_get_state", "wavepp_mpu_destroy",
@@ -103,6 +113,17 @@ class _KdaBatch(ctypes.Structure):
 class _KdaInfo(ctypes.Structure):
     _fields_ = [("total_tokens", ctypes.c_int64), ("num_items", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
                 ("metadata_bytes", ctypes.c_int64), ("workspace_bytes", ctypes.c_int64)]
+
+
+class _LinShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_heads", "num_qk_heads", "head_dim_k", "head_dim_v", "num_state_slots",
+                                               "alpha_per_token")] + [("scale", ctypes.c_float)]
+
+
+class _LinInfo(ctypes.Structure):
+    _fields_ = [("total_tokens", ctypes.c_int64), ("num_step_items", ctypes.c_int32), ("num_segments", ctypes.c_int32),
+                ("num_partials", ctypes.c_int32), ("block_tokens", ctypes.c_int32), ("metadata_bytes", ctypes.c_int64),
+                ("workspace_bytes", ctypes.c_int64)]
 
 
 class _MpuConfig(ctypes.Structure):
@@ -175,6 +196,18 @@ def load_library(path: str = None) -> ctypes.CDLL:
     lib.wavepp_kda_chunked_prefill.restype = ctypes.c_int
     lib.wavepp_kda_destroy.argtypes = [vp]
     lib.wavepp_kda_destroy.restype = None
+    lib.wavepp_lin_plan.argtypes = [ctypes.POINTER(_LinShape), ctypes.POINTER(_KdaBatch), ctypes.POINTER(vp)]
+    lib.wavepp_lin_plan.restype = ctypes.c_int
+    lib.wavepp_lin_workspace_bytes.argtypes = [vp]
+    lib.wavepp_lin_workspace_bytes.restype = sz
+    lib.wavepp_lin_get_info.argtypes = [vp, ctypes.POINTER(_LinInfo)]
+    lib.wavepp_lin_get_info.restype = ctypes.c_int
+    lib.wavepp_lin_upload.argtypes = [vp, vp, sz, vp]
+    lib.wavepp_lin_upload.restype = ctypes.c_int
+    lib.wavepp_lin_chunked_prefill.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.wavepp_lin_chunked_prefill.restype = ctypes.c_int
+    lib.wavepp_lin_destroy.argtypes = [vp]
+    lib.wavepp_lin_destroy.restype = None
     cfgp, spanp = ctypes.POINTER(_MpuConfig), ctypes.POINTER(_Span)
     lib.wavepp_mpu_budget_ladder.argtypes = [cfgp, ctypes.POINTER(i32), i32]
     lib.wavepp_mpu_create.argtypes = [cfgp, ctypes.POINTER(vp)]
@@ -485,7 +518,8 @@ def q4_append_kv(p: Plan, k_new, v_new, k_pool, v_pool, workspace, stream=None):
                   ("v_pool", v_pool, sh["pool"]))
     _check(load_library().wavepp_q4_append_kv(
         p.handle, _ptr(k_new, bf, "k_new"), _ptr(v_new, bf, "v_new"), _ptr(k_pool, torch.uint8, "k_pool"),
-        _ptr(v_pool, torch.uint8, "v_pool"), _ptr(workspace, name="workspace"), workspace.nbytes, _stream_for(stream, k_new, v_new, k_pool, v_pool, workspace)))
+        _ptr(v_pool, torch.uint8, "v_pool"), _ptr(workspace, name="workspace"), workspace.nbytes,
+        _stream_for(stream, k_new, v_new, k_pool, v_pool, workspace)))
 
 
 def q4_read_kv(p: Plan, k_pool, v_pool, k_out, v_out, workspace, stream=None):
@@ -498,7 +532,8 @@ def q4_read_kv(p: Plan, k_pool, v_pool, k_out, v_out, workspace, stream=None):
                   ("v_out", v_out, sh["v_new"]))
     _check(load_library().wavepp_q4_read_kv(
         p.handle, _ptr(k_pool, torch.uint8, "k_pool"), _ptr(v_pool, torch.uint8, "v_pool"), _ptr(k_out, bf, "k_out"),
-        _ptr(v_out, bf, "v_out"), _ptr(workspace, name="workspace"), workspace.nbytes, _stream_for(stream, k_pool, v_pool, k_out, v_out, workspace)))
+        _ptr(v_out, bf, "v_out"), _ptr(workspace, name="workspace"), workspace.nbytes,
+        _stream_for(stream, k_pool, v_pool, k_out, v_out, workspace)))
 
 
 def q4_chunked_prefill(p: Plan, q, k_pool, v_pool, out, lse, workspace, stream=None):
@@ -597,6 +632,88 @@ def kda_chunked_prefill(p: KdaPlan, q, k, v, alpha, beta, state_pool, out, works
         p.handle, _ptr(q, bf, "q"), _ptr(k, bf, "k"), _ptr(v, bf, "v"), _ptr(alpha, f32, "alpha"),
         _ptr(beta, f32, "beta"), _ptr(state_pool, f32, "state_pool"), _ptr(out, bf, "out"),
         _ptr(workspace, name="workspace"), workspace.nbytes, _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------------
+# Linear attention with a decay for each head
+# ------------------------------------------------------------------------------------------------
+
+class LinPlan:
+    """A validated wave of a linear-attention layer (host object owned by the library)."""
+
+    def __init__(self, handle, shape):
+        self._h = ctypes.c_void_p(handle)
+        self.shape = shape
+        s = shape
+        T, H, Hqk, dk, dv = s["total_tokens"], s["num_heads"], s["num_qk_heads"], s["head_dim_k"], s["head_dim_v"]
+        self._buffers = {"qk": (T, Hqk, dk), "v": (T, H, dv), "alpha": (T, H) if s["alpha_per_token"] else (H,),
+                         "state_pool": (s["num_state_slots"], H, dk, dv)}
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise ValueError("plan was destroyed")
+        return self._h
+
+    @property
+    def workspace_bytes(self) -> int:
+        return int(load_library().wavepp_lin_workspace_bytes(self.handle))
+
+    def info(self) -> dict:
+        info = _LinInfo()
+        _check(load_library().wavepp_lin_get_info(self.handle, ctypes.byref(info)))
+        return {name: int(getattr(info, name)) for name, _ in _LinInfo._fields_}
+
+    def destroy(self):
+        if self._h:
+            load_library().wavepp_lin_destroy(self._h)
+            self._h = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def lin_plan(*, num_heads, num_qk_heads, head_dim_k, head_dim_v, num_state_slots, chunk_lens, state_in, state_out,
+             scale=1.0, alpha_per_token=True) -> LinPlan:
+    """A wave of S_t = alpha_t S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.  alpha is [T, num_heads], or [num_heads] where
+    alpha_per_token is false; heads share q and k in groups of num_heads / num_qk_heads."""
+    lib = load_library()
+    chunk = np.ascontiguousarray(chunk_lens, dtype=np.int32)
+    s_in = np.ascontiguousarray(state_in, dtype=np.int32)
+    s_out = np.ascontiguousarray(state_out, dtype=np.int32)
+    if not (chunk.ndim == 1 and chunk.shape == s_in.shape == s_out.shape):
+        raise ValueError("chunk_lens, state_in and state_out must be 1-D of the same length")
+    per_token = int(bool(alpha_per_token))
+    shape = _LinShape(num_heads, num_qk_heads, head_dim_k, head_dim_v, num_state_slots, per_token, float(scale))
+    p32 = ctypes.POINTER(ctypes.c_int32)
+    batch = _KdaBatch(int(chunk.shape[0]), chunk.ctypes.data_as(p32), s_in.ctypes.data_as(p32),
+                      s_out.ctypes.data_as(p32))
+    out = ctypes.c_void_p()
+    _check(lib.wavepp_lin_plan(ctypes.byref(shape), ctypes.byref(batch), ctypes.byref(out)))
+    return LinPlan(out.value, dict(num_heads=int(num_heads), num_qk_heads=int(num_qk_heads), head_dim_k=int(head_dim_k),
+                                   head_dim_v=int(head_dim_v), num_state_slots=int(num_state_slots), scale=float(scale),
+                                   alpha_per_token=bool(per_token), total_tokens=int(chunk.sum())))
+
+
+def lin_upload(p: LinPlan, workspace, stream=None):
+    _check(load_library().wavepp_lin_upload(p.handle, _ptr(workspace, name="workspace"), workspace.nbytes,
+                                            _stream_for(stream, workspace)))
+
+
+def lin_chunked_prefill(p: LinPlan, q, k, v, alpha, state_pool, out, workspace, stream=None):
+    """One layer of the wave: out and the snapshots named by state_out."""
+    bf, f32 = _dtypes()
+    sh = p._buffers
+    _required(q=q, k=k, v=v, alpha=alpha, state_pool=state_pool, out=out)
+    _check_shapes(("q", q, sh["qk"]), ("k", k, sh["qk"]), ("v", v, sh["v"]), ("alpha", alpha, sh["alpha"]),
+                  ("state_pool", state_pool, sh["state_pool"]), ("out", out, sh["v"]))
+    _check(load_library().wavepp_lin_chunked_prefill(
+        p.handle, _ptr(q, bf, "q"), _ptr(k, bf, "k"), _ptr(v, bf, "v"), _ptr(alpha, f32, "alpha"),
+        _ptr(state_pool, f32, "state_pool"), _ptr(out, bf, "out"), _ptr(workspace, name="workspace"), workspace.nbytes,
+        _stream_for(stream, q, k, v, alpha, state_pool, out, workspace)))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -1,0 +1,255 @@
+// Host side of linear attention with a decay for each head: validation of the wave, the work list and the launch.
+//
+// Resume semantics and the rules for slots are those of the KDA layers (kda_host.cpp): a wave's workgroups run
+// concurrently, so a slot that one request writes may be neither read nor written by another.
+#include "wavepp_lin.h"
+#include "internal.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <memory>
+#include <new>
+#include <vector>
+
+using namespace wavepp;
+
+struct wavepp_lin_plan_s {
+  wavepp_lin_shape shape;
+  int64_t total_tokens = 0;
+  uint32_t serial = 0;
+  std::vector<LinItem> steps, segments;
+  std::vector<LinScan> scans;
+  int32_t num_parts = 0, num_ahead = 0;     // partial states, and segments whose own state is computed ahead
+  std::vector<unsigned char> blob;
+  size_t off_steps = 0, off_segments = 0, off_scans = 0, off_parts = 0, off_decay = 0;
+  size_t workspace_bytes = 0;
+};
+
+namespace {
+
+inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+int check_ws(const wavepp_lin_plan_t* plan, void* ws, size_t ws_bytes) {
+  if (!ws) return set_error(WAVEPP_EINVAL, "workspace is NULL");
+  if (reinterpret_cast<uintptr_t>(ws) % 256) return set_error(WAVEPP_EINVAL, "workspace must be 256-byte aligned");
+  if (ws_bytes < plan->workspace_bytes)
+    return set_error(WAVEPP_ENOSPACE, "workspace has %zu bytes, plan needs %zu", ws_bytes, plan->workspace_bytes);
+  return WAVEPP_OK;
+}
+
+// Blocks per segment: enough segments to fill the chip's 512 resident workgroups where the chains alone do not.
+int64_t segment_blocks(const std::vector<int64_t>& blocks, int heads) {
+  int64_t total = 0, longest = 1;
+  for (int64_t b : blocks) total += b, longest = std::max(longest, b);
+  if (int64_t(blocks.size()) * heads >= kNumCu) return longest;
+  return std::max<int64_t>(4, ceil_div(total * heads, 2 * kNumCu));
+}
+
+int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wavepp_lin_plan_t** out) {
+  clear_error();
+  if (!shape || !batch || !out) return set_error(WAVEPP_EINVAL, "null argument");
+  *out = nullptr;
+  const wavepp_lin_shape s = *shape;
+  if (s.num_heads <= 0 || s.num_qk_heads <= 0 || s.head_dim_k <= 0 || s.head_dim_v <= 0 || s.num_state_slots < 0)
+    return set_error(WAVEPP_EINVAL, "non-positive shape field");
+  if (s.num_heads % s.num_qk_heads)
+    return set_error(WAVEPP_EINVAL, "num_heads (%d) is not a multiple of num_qk_heads (%d)", s.num_heads, s.num_qk_heads);
+  if (s.alpha_per_token != 0 && s.alpha_per_token != 1) return set_error(WAVEPP_EINVAL, "alpha_per_token must be 0 or 1");
+  if (!std::isfinite(s.scale)) return set_error(WAVEPP_EINVAL, "scale must be finite");
+  if ((s.head_dim_k != 64 && s.head_dim_k != 128) || (s.head_dim_v != 64 && s.head_dim_v != 128))
+    return set_error(WAVEPP_EUNSUPPORTED, "unsupported head dims (d_k=%d, d_v=%d): each 64 or 128", s.head_dim_k, s.head_dim_v);
+  if (int64_t(s.num_heads) * 128 > INT32_MAX / 4) return set_error(WAVEPP_EINVAL, "too many heads");
+  const int32_t R = batch->num_requests;
+  if (R < 0) return set_error(WAVEPP_EINVAL, "num_requests < 0");
+  if (R > 0 && (!batch->chunk_lens || !batch->state_in || !batch->state_out))
+    return set_error(WAVEPP_EINVAL, "null chunk_lens / state_in / state_out");
+
+  int64_t total = 0;
+  std::vector<int32_t> writer(size_t(s.num_state_slots), -1);
+  for (int32_t r = 0; r < R; ++r) {
+    const int32_t c = batch->chunk_lens[r];
+    if (c < 0) return set_error(WAVEPP_EINVAL, "request %d: negative chunk length %d", r, c);
+    total += c;
+    if (total > INT32_MAX / 2) return set_error(WAVEPP_EINVAL, "too many tokens in the wave");
+    if (c == 0) continue;
+    const int32_t si = batch->state_in[r], so = batch->state_out[r];
+    if (si < -1 || si >= s.num_state_slots)
+      return set_error(WAVEPP_ERANGE, "request %d: state_in %d outside [-1, %d)", r, si, s.num_state_slots);
+    if (so < 0 || so >= s.num_state_slots)
+      return set_error(WAVEPP_ERANGE, "request %d: state_out %d outside [0, %d)", r, so, s.num_state_slots);
+    if (writer[so] >= 0)
+      return set_error(WAVEPP_EALIAS, "requests %d and %d both write snapshot slot %d", writer[so], r, so);
+    writer[so] = r;
+  }
+  for (int32_t r = 0; r < R; ++r) {
+    if (batch->chunk_lens[r] == 0) continue;
+    const int32_t si = batch->state_in[r];
+    if (si >= 0 && writer[si] >= 0 && writer[si] != r)
+      return set_error(WAVEPP_EALIAS, "request %d resumes from slot %d, which request %d writes", r, si, writer[si]);
+  }
+
+  std::unique_ptr<wavepp_lin_plan_t> plan(new (std::nothrow) wavepp_lin_plan_t());
+  if (!plan) return set_error(WAVEPP_EINVAL, "out of host memory");
+  plan->shape = s;
+  plan->total_tokens = total;
+  plan->serial = next_serial();
+  std::vector<int64_t> blocks;
+  for (int32_t r = 0; r < R; ++r)
+    if (batch->chunk_lens[r] > kLinStepTokens) blocks.push_back(ceil_div(batch->chunk_lens[r], kLinBlock));
+  const int64_t per = blocks.empty() ? 1 : segment_blocks(blocks, s.num_heads);
+  std::vector<LinItem> last;            // segments without a partial state of their own
+  int64_t cu = 0, parts = 0;
+  for (int32_t r = 0; r < R; ++r) {
+    const int64_t c = batch->chunk_lens[r];
+    LinItem it{};
+    it.cu = int32_t(cu);
+    it.len = int32_t(c);
+    it.state_in = batch->state_in ? batch->state_in[r] : -1;
+    it.state_out = batch->state_out ? batch->state_out[r] : -1;
+    it.part_in = it.part_out = -1;
+    cu += c;
+    if (c == 0) continue;
+    if (c <= kLinStepTokens) {
+      plan->steps.push_back(it);
+      continue;
+    }
+    const int64_t n = ceil_div(c, kLinBlock), pieces = ceil_div(n, per), each = ceil_div(n, pieces);
+    const int64_t count = ceil_div(n, each);
+    // the last segment may end before the first has read its start, so a slot that is resumed in place is copied first
+    const bool copied = count > 1 && it.state_in >= 0 && it.state_in == it.state_out;
+    const int32_t start = copied ? int32_t(parts + count - 1) : -1;
+    if (count > 1) plan->scans.push_back(LinScan{it.state_in, int32_t(parts), int32_t(count - 1), start});
+    for (int64_t g = 0; g < count; ++g) {
+      LinItem x = it;
+      x.cu = int32_t(it.cu + g * each * kLinBlock);
+      x.len = int32_t(std::min(c - g * each * kLinBlock, each * kLinBlock));
+      if (g > 0 || copied) {
+        x.state_in = -1;
+        x.part_in = g > 0 ? int32_t(parts + g - 1) : start;
+      }
+      if (g + 1 < count) {
+        x.state_out = -1;
+        x.part_out = int32_t(parts + g);
+        plan->segments.push_back(x);
+      } else {
+        last.push_back(x);
+      }
+    }
+    parts += count - 1 + copied;
+    if (parts > INT32_MAX / 4) return set_error(WAVEPP_EINVAL, "wave too large");
+  }
+  plan->num_parts = int32_t(parts);
+  plan->num_ahead = int32_t(plan->segments.size());
+  // longest first within each kind, so that the last workgroups to start are short
+  const auto longer = [](const LinItem& a, const LinItem& b) { return a.len > b.len; };
+  std::stable_sort(plan->segments.begin(), plan->segments.end(), longer);
+  std::stable_sort(last.begin(), last.end(), longer);
+  std::stable_sort(plan->steps.begin(), plan->steps.end(), longer);
+  plan->segments.insert(plan->segments.end(), last.begin(), last.end());
+  const int64_t most = std::max({int64_t(plan->segments.size()), int64_t(plan->steps.size())});
+  if (most * s.num_heads > INT32_MAX / 64) return set_error(WAVEPP_EINVAL, "too many workgroups");
+
+  plan->off_steps = sizeof(LinHeader);
+  plan->off_segments = plan->off_steps + sizeof(LinItem) * plan->steps.size();
+  plan->off_scans = plan->off_segments + sizeof(LinItem) * plan->segments.size();
+  plan->blob.assign(plan->off_scans + sizeof(LinScan) * plan->scans.size(), 0);
+  LinHeader h{kLinMagic, plan->serial, int32_t(plan->steps.size()), int32_t(plan->segments.size())};
+  memcpy(plan->blob.data(), &h, sizeof(h));
+  auto put = [&](size_t off, const auto& v) {
+    if (!v.empty()) memcpy(plan->blob.data() + off, v.data(), sizeof(v[0]) * v.size());
+  };
+  put(plan->off_steps, plan->steps);
+  put(plan->off_segments, plan->segments);
+  put(plan->off_scans, plan->scans);
+  plan->off_parts = align_up(plan->blob.size(), 256);
+  const size_t states = size_t(parts) * size_t(s.num_heads);
+  plan->off_decay = plan->off_parts + align_up(states * size_t(s.head_dim_k) * size_t(s.head_dim_v) * sizeof(float), 256);
+  plan->workspace_bytes = plan->off_decay + align_up(states * sizeof(float), 256);
+  *out = plan.release();
+  return WAVEPP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int wavepp_lin_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wavepp_lin_plan_t** out) {
+  try {
+    return make_plan(shape, batch, out);
+  } catch (const std::exception&) {
+    return set_error(WAVEPP_EINVAL, "out of host memory");
+  }
+}
+
+size_t wavepp_lin_workspace_bytes(const wavepp_lin_plan_t* plan) { return plan ? plan->workspace_bytes : 0; }
+
+int wavepp_lin_get_info(const wavepp_lin_plan_t* plan, wavepp_lin_info* info) {
+  if (!plan || !info) return set_error(WAVEPP_EINVAL, "null argument");
+  info->total_tokens = plan->total_tokens;
+  info->num_step_items = int32_t(plan->steps.size());
+  info->num_segments = int32_t(plan->segments.size());
+  info->num_partials = plan->num_parts;
+  info->block_tokens = kLinBlock;
+  info->metadata_bytes = int64_t(plan->blob.size());
+  info->workspace_bytes = int64_t(plan->workspace_bytes);
+  return WAVEPP_OK;
+}
+
+int wavepp_lin_upload(const wavepp_lin_plan_t* plan, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  clear_error();
+  if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
+  int st = check_ws(plan, workspace, ws_bytes);
+  if (st) return st;
+  st = stage_and_copy(plan->blob.data(), plan->blob.size(), workspace, stream);
+  if (st) return st;
+  note_upload(workspace, plan->serial);
+  return WAVEPP_OK;
+}
+
+int wavepp_lin_chunked_prefill(const wavepp_lin_plan_t* plan, const void* q, const void* k, const void* v,
+                               const float* alpha, float* state_pool, void* out, void* workspace, size_t ws_bytes,
+                               hipStream_t stream) {
+  clear_error();
+  if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
+  int st = check_ws(plan, workspace, ws_bytes);
+  if (st) return st;
+  if (plan->total_tokens == 0) return WAVEPP_OK;
+  st = require_upload(workspace, plan->serial, "wavepp_lin_upload");
+  if (st) return st;
+  if (!q || !k || !v || !alpha || !state_pool || !out)
+    return set_error(WAVEPP_EINVAL, "q / k / v / alpha / state_pool / out is NULL");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(state_pool) || !aligned16(out) ||
+      (reinterpret_cast<uintptr_t>(alpha) & 3))
+    return set_error(WAVEPP_EINVAL, "device buffers must be 16-byte aligned (alpha 4-byte)");
+  auto* base = static_cast<unsigned char*>(workspace);
+  LinDevPlan d{};
+  d.hdr = reinterpret_cast<const LinHeader*>(base);
+  d.steps = reinterpret_cast<const LinItem*>(base + plan->off_steps);
+  d.segments = reinterpret_cast<const LinItem*>(base + plan->off_segments);
+  d.scans = reinterpret_cast<const LinScan*>(base + plan->off_scans);
+  d.parts = reinterpret_cast<float*>(base + plan->off_parts);
+  d.part_decay = reinterpret_cast<float*>(base + plan->off_decay);
+  d.serial = plan->serial;
+  d.num_steps = int32_t(plan->steps.size());
+  d.num_segments = int32_t(plan->segments.size());
+  d.num_ahead = plan->num_ahead;
+  d.num_scans = int32_t(plan->scans.size());
+  d.num_heads = plan->shape.num_heads;
+  d.num_qk_heads = plan->shape.num_qk_heads;
+  d.head_dim_k = plan->shape.head_dim_k;
+  d.head_dim_v = plan->shape.head_dim_v;
+  d.alpha_per_token = plan->shape.alpha_per_token;
+  d.scale = plan->shape.scale;
+  const hipError_t e = launch_lin(d, q, k, v, alpha, state_pool, out, stream);
+  return e == hipSuccess ? WAVEPP_OK : set_hip_error(e, "linear attention launch");
+}
+
+void wavepp_lin_destroy(wavepp_lin_plan_t* plan) { delete plan; }
+
+}  // extern "C"

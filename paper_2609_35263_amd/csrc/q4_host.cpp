@@ -3,7 +3,7 @@
 #include "internal.h"
 #include "plan.h"
 
-#include <new>
+#include <exception>
 
 using namespace wavepp;
 
@@ -42,7 +42,7 @@ size_t wavepp_q4_page_bytes(int32_t head_dim, int32_t page_size) {
 int wavepp_q4_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, wavepp_plan** out) {
   try {
     return plan_wave(shape, batch, max_splits, true, out);
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {
     return set_error(WAVEPP_EINVAL, "out of host memory");
   }
 }
