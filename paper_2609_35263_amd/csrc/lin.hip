@@ -7,11 +7,12 @@
 //   O = scale (diag(lam) Q S0 + ((Q K^T) * D) V),      S = lam_64 S0 + K^T diag(D[64][.]) V.
 // All factors are products of decays, never quotients, so a decay of zero (or a tiny one) needs no special case.
 //
-// A workgroup runs one segment of one (request, head), block after block; wave w of its d_v / 32 owns the state's
-// columns 32 w .. 32 w + 31 as 32 x 32 fp32 accumulator tiles.  The accumulator layout of v_mfma_f32_32x32x16_bf16 (lane =
-// column, 16 rows a lane) is that of an operand whose contraction runs over those rows in a permuted order, so
-// the state feeds O^T = S0^T Q^T, and each wave's own logits feed O^T += V^T P^T, from registers; Q and K rows
-// are read from LDS in that order, V and K^T by transposing LDS reads.
+// A workgroup runs one segment of one (request, head), block after block; wave w of its d_v / 16 owns the state's
+// columns 16 w .. 16 w + 15 as 16 x 16 fp32 accumulator tiles.  The accumulator layout of v_mfma_f32_16x16x32_bf16 (lane =
+// column, four rows a lane) is that of an operand whose contraction runs over the rows of two tiles in a permuted
+// order, so the state feeds O^T = S0^T Q^T from registers, Q rows being read from LDS in that order; V and K^T
+// are read by transposing LDS reads.  The ten 16 x 16 tiles of (Q K^T) * D on and under the diagonal are shared out over
+// the waves and go through LDS.  The next block's rows are loaded while a block is worked on.
 #include <hip/hip_runtime.h>
 
 #include "device.h"
@@ -32,16 +33,51 @@ __device__ __forceinline__ bf16x8 cat(bf16x4 a, bf16x4 b) {
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// Registers 8 kk .. 8 kk + 7 of an accumulator tile in bf16: an operand whose contraction runs over those rows.
-__device__ __forceinline__ bf16x8 acc_operand(const f32x16& acc, int kk) {
+// Two accumulator tiles in bf16: an operand whose contraction runs over their 32 rows, slot e of lane group g being
+// row 4 g + e of the first and 4 g + e - 4 of the second.
+__device__ __forceinline__ bf16x8 acc_operand(const f32x4& a, const f32x4& b) {
   bf16x8 r;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r[e] = static_cast<__bf16>(acc[8 * kk + e]);
+  for (int e = 0; e < 4; ++e) r[e] = static_cast<__bf16>(a[e]), r[4 + e] = static_cast<__bf16>(b[e]);
   return r;
+}
+
+// The value of another lane of the same 16; where there is none, 1.
+template <int CTRL>
+__device__ __forceinline__ float row_or_one(float x) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0x3F800000, __float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+constexpr int kRowShl = 0x100, kRowShr = 0x110, kRowBcast = 0x150;   // + distance, or the lane broadcast
+
+// Products of x over this lane and those before it in its 16 lanes.
+__device__ __forceinline__ float row_products(float x) {
+  x *= row_or_one<kRowShr + 1>(x);
+  x *= row_or_one<kRowShr + 2>(x);
+  x *= row_or_one<kRowShr + 4>(x);
+  x *= row_or_one<kRowShr + 8>(x);
+  return x;
+}
+// The same over the lanes after it.
+__device__ __forceinline__ float row_products_after(float x) {
+  x = row_or_one<kRowShl + 1>(x);
+  x *= row_or_one<kRowShl + 1>(x);
+  x *= row_or_one<kRowShl + 2>(x);
+  x *= row_or_one<kRowShl + 4>(x);
+  x *= row_or_one<kRowShl + 8>(x);
+  return x;
+}
+
+// Row l of a lower-triangular 16 x 16 table in lane l of each 16: d[j] = a[j + 1] ... a[l], 1 at j = l, 0 above.
+template <int J = 15>
+__device__ __forceinline__ void row_table(float a, int l, float x, float (&d)[16]) {
+  if constexpr (J < 15) x *= row_or_one<kRowBcast + J + 1>(a);
+  if (l == J) x = 1.0f;
+  d[J] = l < J ? 0.0f : x;
+  if constexpr (J > 0) row_table<J - 1>(a, l, x, d);
 }
 
 // Where a segment starts: a partial state, a snapshot, or nothing.
@@ -56,37 +92,44 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 // Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, bool AHEAD>
-__global__ __launch_bounds__(DV * 2, 2) void lin_blocks_kernel(LinDevPlan p, const __bf16* __restrict__ q,
+__global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, const __bf16* __restrict__ q,
                                                                const __bf16* __restrict__ k,
                                                                const __bf16* __restrict__ v,
                                                                const float* __restrict__ alpha, float* pool,
                                                                __bf16* __restrict__ out) {
-  constexpr int NW = DV / 32, NT = NW * 64;
-  constexpr int KS = DK + 8, VS = DV + 32, DS = kC + 4;
+  constexpr int NW = DV / 16, NT = NW * 64;
+  // Row strides in LDS.  Q: 8-byte reads of 16 rows on distinct banks.  K, V: transposed reads of 4 rows x 32 bytes
+  // on distinct banks.  P: 16-byte reads of 8 rows on distinct banks.
+  constexpr int QS = DK + 8, KS = DK + 16, VS = DV + 16, PS = kC + 8;
   constexpr int KL = kC * DK / 8 / NT, VL = kC * DV / 8 / NT;     // 16-byte pieces per thread and block
-  constexpr int CT = DK / 32;                                     // row tiles of the state
-  __shared__ __attribute__((aligned(16))) __bf16 qs[AHEAD ? 8 : kC * KS];
+  constexpr int CT = DK / 16;                                     // row tiles of the state
+  __shared__ __attribute__((aligned(16))) __bf16 qs[AHEAD ? 8 : kC * QS];
   __shared__ __attribute__((aligned(16))) __bf16 ks[kC * KS];
   __shared__ __attribute__((aligned(16))) __bf16 vs[kC * VS];
-  __shared__ __attribute__((aligned(16))) float dm[AHEAD ? 4 : kC * DS];   // D
-  __shared__ __attribute__((aligned(16))) float al[kC], lam[kC], wt[kC];   // alpha, lam, D[63]
+  __shared__ __attribute__((aligned(16))) __bf16 pm[AHEAD ? 8 : kC * PS];     // (Q K^T) * D
+  __shared__ __attribute__((aligned(16))) float run[4][kC];                   // [u][i]: alpha_{16 u} ... alpha_i
+  __shared__ __attribute__((aligned(16))) float rest[kC], wt[kC];             // alpha after j: in its 16, in the block
+  __shared__ __attribute__((aligned(16))) float diag[AHEAD ? 4 : kC * 16];    // D's 16 x 16 tiles on the diagonal
 
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
   const LinItem it = p.segments[blockIdx.x / H];
   const int head = blockIdx.x % H, qk_head = head / (H / Hqk);
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, hf = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  f32x16 S[CT];
+  f32x4 S[CT];                           // tile c, lane: rows 16 c + 4 g .. + 3 of column 16 wave + l16
 #pragma unroll
-  for (int c = 0; c < CT; ++c) S[c] = f32x16{};
+  for (int c = 0; c < CT; ++c) S[c] = f32x4{};
   if (!AHEAD) {
     if (const float* s0 = start_of(p, it, pool, head)) {
 #pragma unroll
       for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) S[c][r] = s0[(32 * c + 8 * (r >> 2) + 4 * hf + (r & 3)) * DV + 32 * wave + col];
+        for (int r = 0; r < 4; ++r) S[c][r] = s0[(16 * c + 4 * g + r) * DV + 16 * wave + l16];
     }
+    // the tiles above the diagonal that the products with V run over
+    for (int i = tid; i < 32 * 16; i += NT) pm[(i / 256 * 32 + i / 16 % 16) * PS + i / 256 * 32 + 16 + i % 16] = __bf16(0.0f);
   }
 
   u32x4 qreg[AHEAD ? 1 : KL], kreg[KL], vreg[VL];
@@ -124,7 +167,7 @@ __global__ __launch_bounds__(DV * 2, 2) void lin_blocks_kernel(LinDevPlan p, con
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
       const int c = tid + NT * i, row = c / (DK / 8), at = c % (DK / 8) * 8;
-      if (!AHEAD) *reinterpret_cast<u32x4*>(&qs[AHEAD ? 0 : row * KS + at]) = row < n ? qreg[AHEAD ? 0 : i] : u32x4{};
+      if (!AHEAD) *reinterpret_cast<u32x4*>(&qs[AHEAD ? 0 : row * QS + at]) = row < n ? qreg[AHEAD ? 0 : i] : u32x4{};
       *reinterpret_cast<u32x4*>(&ks[row * KS + at]) = row < n ? kreg[i] : u32x4{};
     }
 #pragma unroll
@@ -132,135 +175,89 @@ __global__ __launch_bounds__(DV * 2, 2) void lin_blocks_kernel(LinDevPlan p, con
       const int c = tid + NT * i, row = c / (DV / 8), at = c % (DV / 8) * 8;
       *reinterpret_cast<u32x4*>(&vs[row * VS + at]) = row < n ? vreg[i] : u32x4{};
     }
+    // products of decays: every wave has the block's 64 in its lanes, four waves make a part each
     const float a = lane < n ? areg : 1.0f;
-    // D: wave w the keys 16 w .. 16 w + 15 (waves of a narrower head two such groups), lane i the query
-    float g = a;                         // products of the decays up to this lane's
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) {
-      const float o = __shfl_up(g, s);
-      if (lane >= s) g *= o;
-    }
-    if (wave == 0) {
-      lam[lane] = g;
-      al[lane] = a;
-    }
-    total *= __shfl(g, 63);
-    if (AHEAD) {
-      if (wave == 0) {
-        float b = __shfl_down(a, 1);     // products of the decays after this lane's
-        if (lane == 63) b = 1.0f;
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-          const float o = __shfl_down(b, s);
-          if (lane + s < 64) b *= o;
-        }
-        wt[lane] = b;
+    if (wave < 4) {
+      const float x = row_products(a);
+      const float x0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 15));
+      const float x1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 31));
+      const float x2 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 47));
+      const float x3 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
+      float before = 1.0f;
+      if (g > 0 && wave <= 0) before *= x0;
+      if (g > 1 && wave <= 1) before *= x1;
+      if (g > 2 && wave <= 2) before *= x2;
+      run[wave][lane] = before * x;
+      total *= x0 * x1 * x2 * x3;
+      if (wave == 1 || AHEAD) {
+        const float y = row_products_after(a);
+        rest[lane] = y;
+        float after = 1.0f;
+        if (g < 3) after *= x3;
+        if (g < 2) after *= x2;
+        if (g < 1) after *= x1;
+        wt[lane] = y * after;
       }
-    } else {
-#pragma unroll
-      for (int j0 = 16 * wave; j0 < 64; j0 += 16 * NW) {
-        float x = lane >= j0 + 16 ? a : 1.0f;              // products from key j0 + 16 up to this lane's
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-          const float o = __shfl_up(x, s);
-          if (lane >= s) x *= o;
-        }
-        if (lane < j0 + 15) x = 0.0f;
+      if (!AHEAD && wave == 2) {
         float d[16];
-#pragma unroll
-        for (int j = 15; j >= 0; --j) {
-          if (j < 15) x *= __shfl(a, j0 + j + 1);
-          if (lane == j0 + j) x = 1.0f;
-          d[j] = lane < j0 + j ? 0.0f : x;
-        }
+        row_table(a, l16, 0.0f, d);
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(&dm[AHEAD ? 0 : lane * DS + j0 + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
+          *reinterpret_cast<f32x4*>(&diag[AHEAD ? 0 : lane * 16 + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
       }
     }
     __syncthreads();
     if (t0 + n < it.len) load(t0 + n);
 
-    const __bf16* vl = &vs[(4 * hf + (lane & 15) / 4) * VS + 32 * wave + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)];
-    bf16x8 vf[4];                        // V^T of this wave's columns: tokens 16 t + 8 (e / 4) + 4 hf + e % 4
-#pragma unroll
-    for (int t = 0; t < 4; ++t) vf[t] = cat(lds_read_tr(vl + 16 * t * VS), lds_read_tr(vl + (16 * t + 8) * VS));
-
+    f32x4 o[4];                          // O^T: columns' rows 4 g .. + 3 of tokens 16 i + l16
     if constexpr (!AHEAD) {
-      f32x16 o[2] = {f32x16{}, f32x16{}};                  // O^T: tokens 0-31 and 32-63
-      f32x16 s00 = f32x16{}, s01 = f32x16{}, s11 = f32x16{};   // K Q^T: key half, query half
-#pragma unroll
-      for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-          const int at = 32 * c + 16 * kk + 4 * hf;
-          auto row = [&](const __bf16* m, int r) {
-            const __bf16* x = m + r * KS + at;
-            return cat(*reinterpret_cast<const bf16x4*>(x), *reinterpret_cast<const bf16x4*>(x + 8));
-          };
-          const bf16x8 q0 = row(qs, col), q1 = row(qs, 32 + col), k0 = row(ks, col), k1 = row(ks, 32 + col);
-          const bf16x8 st = acc_operand(S[c], kk);
-          o[0] = mfma(st, q0, o[0]);
-          o[1] = mfma(st, q1, o[1]);
-          s00 = mfma(k0, q0, s00);
-          s01 = mfma(k0, q1, s01);
-          s11 = mfma(k1, q1, s11);
-        }
-      const float l0 = lam[col], l1 = lam[32 + col];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[0][r] *= l0, o[1][r] *= l1;
-      // the weights of the keys for this lane's two queries; above the diagonal nothing, whatever the product was
-      auto weigh = [&](f32x16& s, int i0, int j0) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const f32x4 d = *reinterpret_cast<const f32x4*>(&dm[(i0 + col) * DS + j0 + 8 * u + 4 * hf]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = s[4 * u + e] * d[e];
-            s[4 * u + e] = i0 != j0 || 8 * u + 4 * hf + e <= col ? x : 0.0f;
-          }
-        }
+      auto row = [&](const __bf16* m, int at) {
+        return cat(*reinterpret_cast<const bf16x4*>(m + at), *reinterpret_cast<const bf16x4*>(m + at + 16));
       };
-      weigh(s00, 0, 0);
-      weigh(s01, 32, 0);
-      weigh(s11, 32, 32);
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        o[0] = mfma(vf[t], acc_operand(s00, t), o[0]);
-        o[1] = mfma(vf[t], acc_operand(s01, t), o[1]);
-        o[1] = mfma(vf[2 + t], acc_operand(s11, t), o[1]);
+      for (int i = 0; i < 4; ++i) o[i] = f32x4{};
+#pragma unroll
+      for (int s = 0; s < CT / 2; ++s) {
+        const bf16x8 st = acc_operand(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = mfma(st, row(qs, (16 * i + l16) * QS + 32 * s + 4 * g), o[i]);
       }
-      // O^T through this wave's columns of V in LDS (its reads of them are done) to rows of 64 bytes
-      __bf16* mine = &vs[32 * wave];
+      for (int tile = wave; tile < 10; tile += NW) {       // (queries ti, keys tj), ti >= tj
+        const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
+        f32x4 x = f32x4{};                                 // K Q^T: keys 4 g .. + 3 of query l16
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+        for (int s = 0; s < CT / 2; ++s)
+          x = mfma(row(ks, (16 * tj + l16) * KS + 32 * s + 4 * g), row(qs, (16 * ti + l16) * QS + 32 * s + 4 * g), x);
+        bf16x4 y;
+        if (ti == tj) {                                    // above the diagonal nothing, whatever the product was
+          const f32x4 d = *reinterpret_cast<const f32x4*>(&diag[(16 * ti + l16) * 16 + 4 * g]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          bf16x4 x;
+          for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(4 * g + e <= l16 ? x[e] * d[e] : 0.0f);
+        } else {
+          const f32x4 d = *reinterpret_cast<const f32x4*>(&rest[16 * tj + 4 * g]);
+          const float w = run[tj + 1][16 * ti + l16];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][4 * u + e] * p.scale);
-          *reinterpret_cast<bf16x4*>(mine + (32 * i + col) * VS + 8 * u + 4 * hf) = x;
+          for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
         }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 16 * i + lane / 4, at = 8 * (lane & 3);
-        const u32x4 x = *reinterpret_cast<const u32x4*>(mine + row * VS + at);
-        if (row < n)
-          *reinterpret_cast<u32x4*>(out + (int64_t(it.cu + t0 + row) * H + head) * DV + 32 * wave + at) = x;
+        *reinterpret_cast<bf16x4*>(&pm[(16 * ti + l16) * PS + 16 * tj + 4 * g]) = y;
       }
     }
 
+    // V^T of this wave's columns: tokens 32 t + 8 g + e
+    const __bf16* vl = &vs[(8 * g + (l16 >> 2)) * VS + 16 * wave + 4 * (l16 & 3)];
+    bf16x8 vf[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 4) * VS));
     // S = lam_64 S + K^T (w V): the weighted values as two bf16 parts, which leave the state right to 2^-16
-    const float gamma = lam[63];
+    const float gamma = run[0][63];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) S[c][r] *= gamma;
-    const __bf16* kl = &ks[(4 * hf + (lane & 15) / 4) * KS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)];
-    const float* last = AHEAD ? wt : &dm[AHEAD ? 0 : 63 * DS];
+      for (int r = 0; r < 4; ++r) S[c][r] *= gamma;
+    const __bf16* kl = &ks[(8 * g + (l16 >> 2)) * KS + 4 * (l16 & 3)];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(last + 16 * t + 4 * hf), w1 = *reinterpret_cast<const f32x4*>(last + 16 * t + 8 + 4 * hf);
+    for (int t = 0; t < 2; ++t) {
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&wt[32 * t + 8 * g]), w1 = *reinterpret_cast<const f32x4*>(&wt[32 * t + 8 * g + 4]);
       bf16x8 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -270,9 +267,32 @@ __global__ __launch_bounds__(DV * 2, 2) void lin_blocks_kernel(LinDevPlan p, con
       }
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const bf16x8 kt = cat(lds_read_tr(kl + 16 * t * KS + 32 * c), lds_read_tr(kl + (16 * t + 8) * KS + 32 * c));
+        const bf16x8 kt = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 4) * KS + 16 * c));
         S[c] = mfma(kt, hi, S[c]);
         S[c] = mfma(kt, lo, S[c]);
+      }
+    }
+
+    if constexpr (!AHEAD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float l = run[0][16 * i + l16];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] *= l;
+      }
+      __syncthreads();                   // P is whole
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t <= i / 2; ++t)
+          o[i] = mfma(vf[t], *reinterpret_cast<const bf16x8*>(&pm[(16 * i + l16) * PS + 32 * t + 8 * g]), o[i]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        bf16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][e] * p.scale);
+        if (16 * i + l16 < n)
+          *reinterpret_cast<bf16x4*>(out + (int64_t(it.cu + t0 + 16 * i + l16) * H + head) * DV + 16 * wave + 4 * g) = x;
       }
     }
   }
@@ -284,7 +304,7 @@ __global__ __launch_bounds__(DV * 2, 2) void lin_blocks_kernel(LinDevPlan p, con
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) to[(32 * c + 8 * (r >> 2) + 4 * hf + (r & 3)) * DV + 32 * wave + col] = S[c][r];
+      for (int r = 0; r < 4; ++r) to[(16 * c + 4 * g + r) * DV + 16 * wave + l16] = S[c][r];
   }
   if (AHEAD && tid == 0) p.part_decay[int64_t(it.part_out) * H + head] = total;
 }
@@ -376,12 +396,12 @@ hipError_t launch_dims(const LinDevPlan& p, const __bf16* q, const __bf16* k, co
     hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(p.num_steps * H * (DV / 32)), dim3(256), 0, stream, p, q, k, v, alpha,
                        pool, out);
   if (p.num_ahead)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, true>), dim3(p.num_ahead * H), dim3(2 * DV), 0, stream, p, q, k, v, alpha,
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, true>), dim3(p.num_ahead * H), dim3(4 * DV), 0, stream, p, q, k, v, alpha,
                        pool, out);
   if (p.num_scans)
     hipLaunchKernelGGL(lin_scan_kernel, dim3(p.num_scans * H, DK * DV / 1024), dim3(256), 0, stream, p, pool);
   if (p.num_segments)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, false>), dim3(p.num_segments * H), dim3(2 * DV), 0, stream, p, q, k, v,
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, false>), dim3(p.num_segments * H), dim3(4 * DV), 0, stream, p, q, k, v,
                        alpha, pool, out);
   return hipGetLastError();
 }
