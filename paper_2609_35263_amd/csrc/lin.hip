@@ -92,24 +92,28 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 // Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, bool AHEAD>
-__global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, const __bf16* __restrict__ q,
-                                                               const __bf16* __restrict__ k,
-                                                               const __bf16* __restrict__ v,
-                                                               const float* __restrict__ alpha, float* pool,
-                                                               __bf16* __restrict__ out) {
+__global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel(
+    LinDevPlan p, const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+    const float* __restrict__ alpha, float* pool, __bf16* __restrict__ out) {
   constexpr int NW = DV / 16, NT = NW * 64;
-  // Row strides in LDS.  Q: 8-byte reads of 16 rows on distinct banks.  K, V: transposed reads of 4 rows x 32 bytes
-  // on distinct banks.  P: 16-byte reads of 8 rows on distinct banks.
-  constexpr int QS = DK + 8, KS = DK + 16, VS = DV + 16, PS = kC + 8;
+  // LDS layouts, for its 64 banks.  Q's and P's rows keep each 32 of their columns in the order of an operand's slots
+  // (4-column group u of eight at place 2 (u % 4) + u / 4), so one 16-byte read gives an operand, eight rows on distinct
+  // banks.  K, V: transposed reads of 8 rows x 32 bytes on distinct banks.  K's rows with bit 3 set have neighbouring
+  // 16-byte pieces swapped, which puts the 8-byte reads of 16 rows on distinct banks too.
+  constexpr int QS = DK + 8, KS = DK + 16, VS = DV + 16, PS = kC + 8, GS = 20;
   constexpr int KL = kC * DK / 8 / NT, VL = kC * DV / 8 / NT;     // 16-byte pieces per thread and block
   constexpr int CT = DK / 16;                                     // row tiles of the state
-  __shared__ __attribute__((aligned(16))) __bf16 qs[AHEAD ? 8 : kC * QS];
-  __shared__ __attribute__((aligned(16))) __bf16 ks[kC * KS];
-  __shared__ __attribute__((aligned(16))) __bf16 vs[kC * VS];
-  __shared__ __attribute__((aligned(16))) __bf16 pm[AHEAD ? 8 : kC * PS];     // (Q K^T) * D
-  __shared__ __attribute__((aligned(16))) float run[4][kC];                   // [u][i]: alpha_{16 u} ... alpha_i
-  __shared__ __attribute__((aligned(16))) float rest[kC], wt[kC];             // alpha after j: in its 16, in the block
-  __shared__ __attribute__((aligned(16))) float diag[AHEAD ? 4 : kC * 16];    // D's 16 x 16 tiles on the diagonal
+  struct Block {
+    __bf16 q[AHEAD ? 8 : kC * QS];
+    __bf16 k[kC * KS];
+    __bf16 v[kC * VS];
+    __bf16 p[AHEAD ? 8 : kC * PS];     // (Q K^T) * D
+    float run[4][kC];                  // [u][i]: alpha_{16 u} ... alpha_i
+    float rest[kC], wt[kC];            // alpha after j: in its 16, in the block
+    float diag[AHEAD ? 4 : kC * GS];   // D's 16 x 16 tiles on the diagonal
+    int bad[8];                        // per wave: a value of V is not finite
+  };
+  __shared__ __attribute__((aligned(16))) Block blk[2];
 
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
@@ -129,7 +133,10 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, con
         for (int r = 0; r < 4; ++r) S[c][r] = s0[(16 * c + 4 * g + r) * DV + 16 * wave + l16];
     }
     // the tiles above the diagonal that the products with V run over
-    for (int i = tid; i < 32 * 16; i += NT) pm[(i / 256 * 32 + i / 16 % 16) * PS + i / 256 * 32 + 16 + i % 16] = __bf16(0.0f);
+    for (int i = tid; i < 2 * 32 * 16; i += NT) {
+      const int u = i % 512;
+      blk[i / 512].p[AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
+    }
   }
 
   u32x4 qreg[AHEAD ? 1 : KL], kreg[KL], vreg[VL];
@@ -151,32 +158,34 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, con
     }
     areg = t0 + lane < it.len ? alpha[p.alpha_per_token ? int64_t(it.cu + t0 + lane) * H + head : int64_t(head)] : 1.0f;
   };
-
   float total = 1.0f;                    // AHEAD: the segment's decay so far
-  load(0);
-  for (int t0 = 0, n; t0 < it.len; t0 += n) {
-    n = min(kC, it.len - t0);
-    // A value that is not finite times a weight of zero would reach the tokens before it: such a block goes token by
-    // token, in blocks of one.
+  // The loaded rows to LDS, and the products of their decays: every wave has the 64 in its lanes, four make a part each.
+  auto store = [&](Block& b) {
     uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < VL; ++i)
-#pragma unroll
-      for (int u = 0; u < 4; ++u) top = max(top, max(vreg[i][u] & 0x7FFFu, (vreg[i][u] >> 16) & 0x7FFFu));
-    if (__syncthreads_or(top >= 0x7F80u)) n = AHEAD ? n : 1;
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
       const int c = tid + NT * i, row = c / (DK / 8), at = c % (DK / 8) * 8;
-      if (!AHEAD) *reinterpret_cast<u32x4*>(&qs[AHEAD ? 0 : row * QS + at]) = row < n ? qreg[AHEAD ? 0 : i] : u32x4{};
-      *reinterpret_cast<u32x4*>(&ks[row * KS + at]) = row < n ? kreg[i] : u32x4{};
+      if (!AHEAD) {
+        const int u = at / 8 % 4;                          // 4-column groups 2 u and 2 u + 1 of their 32 columns
+        __bf16* to = &b.q[AHEAD ? 0 : row * QS + at / 32 * 32 + u % 2 * 16 + u / 2 * 4];
+        const u32x4 x = qreg[AHEAD ? 0 : i];
+        *reinterpret_cast<u32x2*>(to) = u32x2{x[0], x[1]};
+        *reinterpret_cast<u32x2*>(to + 8) = u32x2{x[2], x[3]};
+      }
+      *reinterpret_cast<u32x4*>(&b.k[row * KS + (at ^ (row & 8))]) = kreg[i];
     }
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
       const int c = tid + NT * i, row = c / (DV / 8), at = c % (DV / 8) * 8;
-      *reinterpret_cast<u32x4*>(&vs[row * VS + at]) = row < n ? vreg[i] : u32x4{};
+      *reinterpret_cast<u32x4*>(&b.v[row * VS + at]) = vreg[i];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) top = max(top, max(vreg[i][u] & 0x7FFFu, (vreg[i][u] >> 16) & 0x7FFFu));
     }
-    // products of decays: every wave has the block's 64 in its lanes, four waves make a part each
-    const float a = lane < n ? areg : 1.0f;
+    if (!AHEAD) {
+      const bool bad = __any(top >= 0x7F80u);
+      if (lane == 0) b.bad[wave] = bad;
+    }
+    const float a = areg;
     if (wave < 4) {
       const float x = row_products(a);
       const float x0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 15));
@@ -187,77 +196,131 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, con
       if (g > 0 && wave <= 0) before *= x0;
       if (g > 1 && wave <= 1) before *= x1;
       if (g > 2 && wave <= 2) before *= x2;
-      run[wave][lane] = before * x;
+      b.run[wave][lane] = before * x;
       total *= x0 * x1 * x2 * x3;
-      if (wave == 1 || AHEAD) {
+      if (wave == 1) {
         const float y = row_products_after(a);
-        rest[lane] = y;
+        b.rest[lane] = y;
         float after = 1.0f;
         if (g < 3) after *= x3;
         if (g < 2) after *= x2;
         if (g < 1) after *= x1;
-        wt[lane] = y * after;
+        b.wt[lane] = y * after;
       }
       if (!AHEAD && wave == 2) {
         float d[16];
         row_table(a, l16, 0.0f, d);
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(&diag[AHEAD ? 0 : lane * 16 + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
+          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
       }
     }
-    __syncthreads();
-    if (t0 + n < it.len) load(t0 + n);
+  };
+  auto operand = [&](const __bf16* m, int at) { return *reinterpret_cast<const bf16x8*>(m + at); };
 
-    f32x4 o[4];                          // O^T: columns' rows 4 g .. + 3 of tokens 16 i + l16
+  // What a block leaves for the step after it: its part of O, V^T of this wave's columns (slot e of lane group g is token
+  // 32 t + 4 g + e, or 16 + 4 g + e - 4 from the fifth on), and whether V has a value that is not finite.
+  f32x4 o[4];                            // O^T: columns' rows 4 g .. + 3 of tokens 16 i + l16
+  bf16x8 vf[2];
+  bool bad = false;
+  auto finish = [&](const Block& b, int t0) {              // O += P V, and out
+    if (!bad) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t <= i / 2; ++t) o[i] = mfma(vf[t], operand(b.p, (16 * i + l16) * PS + 32 * t + 8 * g), o[i]);
+    } else {
+      // a value that is not finite, times the zeros above the diagonal, would reach the tokens before it
+      for (int i = 0; i < 4; ++i)
+        for (int j = 0; j <= 16 * i + l16; ++j) {
+          const float w = float(b.p[(16 * i + l16) * PS + j / 32 * 32 + j / 4 % 4 * 8 + j / 16 % 2 * 4 + j % 4]);
+          const bf16x4 x = *reinterpret_cast<const bf16x4*>(&b.v[j * VS + 16 * wave + 4 * g]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float y = o[i][e] + w * float(x[e]);
+            o[i][e] = y;
+          }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][e] * p.scale);
+      if (t0 + 16 * i + l16 < it.len)
+        *reinterpret_cast<bf16x4*>(out + (int64_t(it.cu + t0 + 16 * i + l16) * H + head) * DV + 16 * wave + 4 * g) = x;
+    }
+  };
+
+  // One barrier a block: between two of them a wave finishes the block before (whose P is whole by then), works on the
+  // present one, moves the next one from its registers to the other half of LDS and asks for the one after.
+  load(0);
+  store(blk[0]);
+  if (kC < it.len) load(kC);
+  __syncthreads();
+  for (int t0 = 0, half = 0; t0 < it.len; t0 += kC, half ^= 1) {
+    const Block& b = blk[half];
+    if (!AHEAD && t0 > 0) {
+      finish(blk[half ^ 1], t0 - kC);
+      if (bad) __syncthreads();          // finish read V from what is stored to next
+    }
     if constexpr (!AHEAD) {
-      auto row = [&](const __bf16* m, int at) {
-        return cat(*reinterpret_cast<const bf16x4*>(m + at), *reinterpret_cast<const bf16x4*>(m + at + 16));
-      };
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = f32x4{};
 #pragma unroll
       for (int s = 0; s < CT / 2; ++s) {
         const bf16x8 st = acc_operand(S[2 * s], S[2 * s + 1]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = mfma(st, row(qs, (16 * i + l16) * QS + 32 * s + 4 * g), o[i]);
+        for (int i = 0; i < 4; ++i) o[i] = mfma(st, operand(b.q, (16 * i + l16) * QS + 32 * s + 8 * g), o[i]);
       }
       for (int tile = wave; tile < 10; tile += NW) {       // (queries ti, keys tj), ti >= tj
         const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
         f32x4 x = f32x4{};                                 // K Q^T: keys 4 g .. + 3 of query l16
 #pragma unroll
         for (int s = 0; s < CT / 2; ++s)
-          x = mfma(row(ks, (16 * tj + l16) * KS + 32 * s + 4 * g), row(qs, (16 * ti + l16) * QS + 32 * s + 4 * g), x);
+        {
+          const __bf16* kr = &b.k[(16 * tj + l16) * KS + 32 * s + ((4 * g) ^ (l16 & 8))];
+          x = mfma(cat(*reinterpret_cast<const bf16x4*>(kr), *reinterpret_cast<const bf16x4*>(kr + 16)),
+                   operand(b.q, (16 * ti + l16) * QS + 32 * s + 8 * g), x);
+        }
         bf16x4 y;
         if (ti == tj) {                                    // above the diagonal nothing, whatever the product was
-          const f32x4 d = *reinterpret_cast<const f32x4*>(&diag[(16 * ti + l16) * 16 + 4 * g]);
+          const f32x4 d = *reinterpret_cast<const f32x4*>(&b.diag[(16 * ti + l16) * GS + 4 * g]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(4 * g + e <= l16 ? x[e] * d[e] : 0.0f);
         } else {
-          const f32x4 d = *reinterpret_cast<const f32x4*>(&rest[16 * tj + 4 * g]);
-          const float w = run[tj + 1][16 * ti + l16];
+          const f32x4 d = *reinterpret_cast<const f32x4*>(&b.rest[16 * tj + 4 * g]);
+          const float w = b.run[tj + 1][16 * ti + l16];
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
         }
-        *reinterpret_cast<bf16x4*>(&pm[(16 * ti + l16) * PS + 16 * tj + 4 * g]) = y;
+        *reinterpret_cast<bf16x4*>(&blk[half].p[(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
+      }
+      uint32_t any = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) any |= b.bad[w];
+      bad = __builtin_amdgcn_readfirstlane(any) != 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float l = b.run[0][16 * i + l16];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][e] *= l;
       }
     }
 
-    // V^T of this wave's columns: tokens 32 t + 8 g + e
-    const __bf16* vl = &vs[(8 * g + (l16 >> 2)) * VS + 16 * wave + 4 * (l16 & 3)];
-    bf16x8 vf[2];
+    const __bf16* vl = &b.v[(4 * g + (l16 >> 2)) * VS + 16 * wave + 4 * (l16 & 3)];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 4) * VS));
+    for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 16) * VS));
     // S = lam_64 S + K^T (w V): the weighted values as two bf16 parts, which leave the state right to 2^-16
-    const float gamma = run[0][63];
+    const float gamma = b.run[0][63];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int r = 0; r < 4; ++r) S[c][r] *= gamma;
-    const __bf16* kl = &ks[(8 * g + (l16 >> 2)) * KS + 4 * (l16 & 3)];
+    const __bf16* kl = &b.k[(4 * g + (l16 >> 2)) * KS + ((4 * (l16 & 3)) ^ (4 * g & 8))];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&wt[32 * t + 8 * g]), w1 = *reinterpret_cast<const f32x4*>(&wt[32 * t + 8 * g + 4]);
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 4 * g]), w1 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 16 + 4 * g]);
       bf16x8 hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -267,34 +330,20 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(LinDevPlan p, con
       }
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const bf16x8 kt = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 4) * KS + 16 * c));
+        const bf16x8 kt = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 16) * KS + 16 * c));
         S[c] = mfma(kt, hi, S[c]);
         S[c] = mfma(kt, lo, S[c]);
       }
     }
-
-    if constexpr (!AHEAD) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float l = run[0][16 * i + l16];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][e] *= l;
-      }
-      __syncthreads();                   // P is whole
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t <= i / 2; ++t)
-          o[i] = mfma(vf[t], *reinterpret_cast<const bf16x8*>(&pm[(16 * i + l16) * PS + 32 * t + 8 * g]), o[i]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        bf16x4 x;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][e] * p.scale);
-        if (16 * i + l16 < n)
-          *reinterpret_cast<bf16x4*>(out + (int64_t(it.cu + t0 + 16 * i + l16) * H + head) * DV + 16 * wave + 4 * g) = x;
-      }
+    if (t0 + kC < it.len) {
+      store(blk[half ^ 1]);
+      if (t0 + 2 * kC < it.len) load(t0 + 2 * kC);
     }
+    __syncthreads();
+  }
+  if (!AHEAD) {
+    const int blocks = (it.len + kC - 1) / kC;
+    finish(blk[(blocks - 1) & 1], (blocks - 1) * kC);
   }
 
   const int64_t size = int64_t(DK) * DV;
