@@ -23,6 +23,8 @@
 namespace wavepp {
 namespace {
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 constexpr int kC = kLinBlock;
 
 __device__ __forceinline__ bool lin_meta_ok(const LinDevPlan& p) {
@@ -80,6 +82,18 @@ __device__ __forceinline__ void row_table(float a, int l, float x, float (&d)[16
   if constexpr (J > 0) row_table<J - 1>(a, l, x, d);
 }
 
+// A buffer descriptor of `bytes` from a uniform address: loads behind them give zero, stores behind them do nothing.
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rows(const T* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00027000);
+}
+
+// An item by scalar loads (the kernels never write the metadata), so that the compiler knows it is uniform.
+__device__ __forceinline__ LinItem item_at(const LinItem* at) {
+  struct Halves { u32x4 a, b; } x = {const_load(reinterpret_cast<const u32x4*>(at)), const_load(reinterpret_cast<const u32x4*>(at) + 1)};
+  return __builtin_bit_cast(LinItem, x);
+}
+
 // Where a segment starts: a partial state, a snapshot, or nothing.
 __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinItem& it, const float* pool, int head) {
   const int64_t size = int64_t(p.head_dim_k) * p.head_dim_v;
@@ -92,7 +106,7 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 // Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, bool AHEAD>
-__global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel(
+__global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     LinDevPlan p, const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const float* __restrict__ alpha, float* pool, __bf16* __restrict__ out) {
   constexpr int NW = DV / 16, NT = NW * 64;
@@ -103,21 +117,24 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
   constexpr int QS = DK + 8, KS = DK + 16, VS = DV + 16, PS = kC + 8, GS = 20;
   constexpr int KL = kC * DK / 8 / NT, VL = kC * DV / 8 / NT;     // 16-byte pieces per thread and block
   constexpr int CT = DK / 16;                                     // row tiles of the state
-  struct Block {
+  constexpr int BUF = DV == 128 ? 2 : 1;                          // blocks in LDS
+  struct alignas(16) Block {
     __bf16 q[AHEAD ? 8 : kC * QS];
     __bf16 k[kC * KS];
     __bf16 v[kC * VS];
-    __bf16 p[AHEAD ? 8 : kC * PS];     // (Q K^T) * D
-    float run[4][kC];                  // [u][i]: alpha_{16 u} ... alpha_i
-    float rest[kC], wt[kC];            // alpha after j: in its 16, in the block
-    float diag[AHEAD ? 4 : kC * GS];   // D's 16 x 16 tiles on the diagonal
+    float run[3][kC];                  // [u][i]: alpha_{16 (u + 1)} ... alpha_i
+    float lam[kC];                     // scale alpha_0 ... alpha_i
+    float rest[kC], wt[kC];            // alpha after j: in its 16 times scale, in the block
+    float diag[AHEAD ? 4 : kC * GS];   // D's 16 x 16 tiles on the diagonal, times scale
+    float gamma;                       // the block's decay
     int bad[8];                        // per wave: a value of V is not finite
   };
-  __shared__ __attribute__((aligned(16))) Block blk[2];
+  __shared__ __attribute__((aligned(16))) Block blk[BUF];
+  __shared__ __attribute__((aligned(16))) __bf16 pm[2][AHEAD ? 8 : kC * PS];   // scale (Q K^T) * D
 
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
-  const LinItem it = p.segments[blockIdx.x / H];
+  const LinItem it = item_at(p.segments + blockIdx.x / H);
   const int head = blockIdx.x % H, qk_head = head / (H / Hqk);
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -135,57 +152,67 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
     // the tiles above the diagonal that the products with V run over
     for (int i = tid; i < 2 * 32 * 16; i += NT) {
       const int u = i % 512;
-      blk[i / 512].p[AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
+      pm[i / 512][AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
     }
   }
 
-  u32x4 qreg[AHEAD ? 1 : KL], kreg[KL], vreg[VL];
-  float areg = 1.0f;
-  auto load = [&](int t0) {
+  struct Rows {                          // a block on its way from memory
+    u32x4 q[AHEAD ? 1 : KL], k[KL], v[VL];
+    float a;
+  };
+  // Byte offsets of this thread's pieces in a block.  Loads and stores go through buffer descriptors that end with the
+  // segment's last token: what lies behind reads as zero and is not written, and there is no branch around them, so the
+  // compiler knows how many are in flight and waits for the oldest block alone.
+  uint32_t qk_off[KL], v_off[VL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i) qk_off[i] = uint32_t((tid + NT * i) / (DK / 8) * Hqk * DK + (tid + NT * i) % (DK / 8) * 8) * 2;
+#pragma unroll
+  for (int i = 0; i < VL; ++i) v_off[i] = uint32_t((tid + NT * i) / (DV / 8) * H * DV + (tid + NT * i) % (DV / 8) * 8) * 2;
+  const uint32_t a_row = p.alpha_per_token ? uint32_t(H) * 4 : 0;
+  auto load = [&](Rows& x, int t0) {
+    const int rows = __builtin_amdgcn_readfirstlane(max(0, min(kC, it.len - t0)));
+    const int64_t tok = it.cu + min(t0, it.len);
+    const auto qb = block_rows(q + (tok * Hqk + qk_head) * DK, rows * uint32_t(Hqk * DK * 2));
+    const auto kb = block_rows(k + (tok * Hqk + qk_head) * DK, rows * uint32_t(Hqk * DK * 2));
+    const auto vb = block_rows(v + (tok * H + head) * DV, rows * uint32_t(H * DV * 2));
+    const auto ab = block_rows(alpha + (p.alpha_per_token ? tok * H + head : head), p.alpha_per_token ? rows * a_row : 4);
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
-      const int c = tid + NT * i, row = c / (DK / 8), at = c % (DK / 8) * 8;
-      const bool ok = t0 + row < it.len;
-      const int64_t off = (int64_t(it.cu + t0 + row) * Hqk + qk_head) * DK + at;
-      if (!AHEAD) qreg[AHEAD ? 0 : i] = ok ? *reinterpret_cast<const u32x4*>(q + off) : u32x4{};
-      kreg[i] = ok ? *reinterpret_cast<const u32x4*>(k + off) : u32x4{};
+      if (!AHEAD) x.q[AHEAD ? 0 : i] = __builtin_amdgcn_raw_buffer_load_b128(qb, qk_off[i], 0, 0);
+      x.k[i] = __builtin_amdgcn_raw_buffer_load_b128(kb, qk_off[i], 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < VL; ++i) {
-      const int c = tid + NT * i, row = c / (DV / 8), at = c % (DV / 8) * 8;
-      const bool ok = t0 + row < it.len;
-      vreg[i] = ok ? *reinterpret_cast<const u32x4*>(v + (int64_t(it.cu + t0 + row) * H + head) * DV + at) : u32x4{};
-    }
-    areg = t0 + lane < it.len ? alpha[p.alpha_per_token ? int64_t(it.cu + t0 + lane) * H + head : int64_t(head)] : 1.0f;
+    for (int i = 0; i < VL; ++i) x.v[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, v_off[i], 0, 0);
+    x.a = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ab, lane * a_row, 0, 0));
   };
   float total = 1.0f;                    // AHEAD: the segment's decay so far
   // The loaded rows to LDS, and the products of their decays: every wave has the 64 in its lanes, four make a part each.
-  auto store = [&](Block& b) {
-    uint32_t top = 0;
+  auto store = [&](Block& b, const Rows& rows, int t0) {
+    u16x2 top = u16x2{0, 0};
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
       const int c = tid + NT * i, row = c / (DK / 8), at = c % (DK / 8) * 8;
       if (!AHEAD) {
         const int u = at / 8 % 4;                          // 4-column groups 2 u and 2 u + 1 of their 32 columns
         __bf16* to = &b.q[AHEAD ? 0 : row * QS + at / 32 * 32 + u % 2 * 16 + u / 2 * 4];
-        const u32x4 x = qreg[AHEAD ? 0 : i];
+        const u32x4 x = rows.q[AHEAD ? 0 : i];
         *reinterpret_cast<u32x2*>(to) = u32x2{x[0], x[1]};
         *reinterpret_cast<u32x2*>(to + 8) = u32x2{x[2], x[3]};
       }
-      *reinterpret_cast<u32x4*>(&b.k[row * KS + (at ^ (row & 8))]) = kreg[i];
+      *reinterpret_cast<u32x4*>(&b.k[row * KS + (at ^ (row & 8))]) = rows.k[i];
     }
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
       const int c = tid + NT * i, row = c / (DV / 8), at = c % (DV / 8) * 8;
-      *reinterpret_cast<u32x4*>(&b.v[row * VS + at]) = vreg[i];
+      *reinterpret_cast<u32x4*>(&b.v[row * VS + at]) = rows.v[i];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) top = max(top, max(vreg[i][u] & 0x7FFFu, (vreg[i][u] >> 16) & 0x7FFFu));
+      for (int u = 0; u < 4; ++u) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, rows.v[i][u] & 0x7FFF7FFFu));
     }
     if (!AHEAD) {
-      const bool bad = __any(top >= 0x7F80u);
+      const bool bad = __any(max(top[0], top[1]) >= 0x7F80);
       if (lane == 0) b.bad[wave] = bad;
     }
-    const float a = areg;
+    const float a = t0 + lane < it.len ? rows.a : 1.0f;    // no decay behind the last token
     if (wave < 4) {
       const float x = row_products(a);
       const float x0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 15));
@@ -196,11 +223,14 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
       if (g > 0 && wave <= 0) before *= x0;
       if (g > 1 && wave <= 1) before *= x1;
       if (g > 2 && wave <= 2) before *= x2;
-      b.run[wave][lane] = before * x;
-      total *= x0 * x1 * x2 * x3;
+      if (wave > 0) b.run[wave - 1][lane] = before * x;
+      else b.lam[lane] = before * x * p.scale;
+      const float all = x0 * x1 * x2 * x3;
+      total *= all;
+      if (tid == 0) b.gamma = all;
       if (wave == 1) {
         const float y = row_products_after(a);
-        b.rest[lane] = y;
+        b.rest[lane] = y * p.scale;
         float after = 1.0f;
         if (g < 3) after *= x3;
         if (g < 2) after *= x2;
@@ -212,58 +242,47 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
         row_table(a, l16, 0.0f, d);
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]};
+          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]} * p.scale;
       }
     }
   };
   auto operand = [&](const __bf16* m, int at) { return *reinterpret_cast<const bf16x8*>(m + at); };
 
-  // What a block leaves for the step after it: its part of O, V^T of this wave's columns (slot e of lane group g is token
-  // 32 t + 4 g + e, or 16 + 4 g + e - 4 from the fifth on), and whether V has a value that is not finite.
+  // What a block leaves for the step after it: its part of O, and V^T of this wave's columns (slot e of lane group g is
+  // token 32 t + 4 g + e, or 16 + 4 g + e - 4 from the fifth on).
   f32x4 o[4];                            // O^T: columns' rows 4 g .. + 3 of tokens 16 i + l16
   bf16x8 vf[2];
-  bool bad = false;
-  auto finish = [&](const Block& b, int t0) {              // O += P V, and out
-    if (!bad) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t <= i / 2; ++t) o[i] = mfma(vf[t], operand(b.p, (16 * i + l16) * PS + 32 * t + 8 * g), o[i]);
-    } else {
-      // a value that is not finite, times the zeros above the diagonal, would reach the tokens before it
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j <= 16 * i + l16; ++j) {
-          const float w = float(b.p[(16 * i + l16) * PS + j / 32 * 32 + j / 4 % 4 * 8 + j / 16 % 2 * 4 + j % 4]);
-          const bf16x4 x = *reinterpret_cast<const bf16x4*>(&b.v[j * VS + 16 * wave + 4 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float y = o[i][e] + w * float(x[e]);
-            o[i][e] = y;
-          }
-        }
-    }
+  const uint32_t o_off = uint32_t(l16 * H * DV + 16 * wave + 4 * g) * 2;
+  auto put = [&](int t0) {
+    const auto ob = block_rows(out + (int64_t(it.cu + t0) * H + head) * DV, __builtin_amdgcn_readfirstlane(min(kC, it.len - t0)) * uint32_t(H * DV * 2));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       bf16x4 x;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][e] * p.scale);
-      if (t0 + 16 * i + l16 < it.len)
-        *reinterpret_cast<bf16x4*>(out + (int64_t(it.cu + t0 + 16 * i + l16) * H + head) * DV + 16 * wave + 4 * g) = x;
+      for (int e = 0; e < 4; ++e) x[e] = static_cast<__bf16>(o[i][e]);
+      __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, x), ob, o_off + 16 * i * uint32_t(H * DV * 2), 0, 0);
     }
   };
+  auto finish = [&](const __bf16* pb, int t0) {            // O += P V, and out
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t <= i / 2; ++t) o[i] = mfma(vf[t], operand(pb, (16 * i + l16) * PS + 32 * t + 8 * g), o[i]);
+    put(t0);
+  };
 
-  // One barrier a block: between two of them a wave finishes the block before (whose P is whole by then), works on the
-  // present one, moves the next one from its registers to the other half of LDS and asks for the one after.
-  load(0);
-  store(blk[0]);
-  if (kC < it.len) load(kC);
+  // Between two barriers a wave finishes the block before (whose P is whole by then), works on the present one, moves the
+  // next one from its registers to LDS and asks for the one after.  With two buffers that is one barrier a block; one
+  // buffer takes another before the move, and leaves room for a second workgroup.
+  Rows rows;
+  load(rows, 0);
+  store(blk[0], rows, 0);
+  load(rows, kC);
   __syncthreads();
+  bool pending = false;
   for (int t0 = 0, half = 0; t0 < it.len; t0 += kC, half ^= 1) {
-    const Block& b = blk[half];
-    if (!AHEAD && t0 > 0) {
-      finish(blk[half ^ 1], t0 - kC);
-      if (bad) __syncthreads();          // finish read V from what is stored to next
-    }
+    const Block& b = blk[half % BUF];
+    if (pending) finish(pm[half ^ 1], t0 - kC);
     if constexpr (!AHEAD) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = f32x4{};
@@ -290,19 +309,15 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
           for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(4 * g + e <= l16 ? x[e] * d[e] : 0.0f);
         } else {
           const f32x4 d = *reinterpret_cast<const f32x4*>(&b.rest[16 * tj + 4 * g]);
-          const float w = b.run[tj + 1][16 * ti + l16];
+          const float w = b.run[tj][16 * ti + l16];
 #pragma unroll
           for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
         }
-        *reinterpret_cast<bf16x4*>(&blk[half].p[(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
+        *reinterpret_cast<bf16x4*>(&pm[half][(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
       }
-      uint32_t any = 0;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) any |= b.bad[w];
-      bad = __builtin_amdgcn_readfirstlane(any) != 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float l = b.run[0][16 * i + l16];
+        const float l = b.lam[16 * i + l16];
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][e] *= l;
       }
@@ -312,7 +327,7 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
 #pragma unroll
     for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 16) * VS));
     // S = lam_64 S + K^T (w V): the weighted values as two bf16 parts, which leave the state right to 2^-16
-    const float gamma = b.run[0][63];
+    const float gamma = b.gamma;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -335,15 +350,36 @@ __global__ __launch_bounds__(DV * 4, AHEAD ? 2 : DV / 64) void lin_blocks_kernel
         S[c] = mfma(kt, lo, S[c]);
       }
     }
-    if (t0 + kC < it.len) {
-      store(blk[half ^ 1]);
-      if (t0 + 2 * kC < it.len) load(t0 + 2 * kC);
+    pending = !AHEAD;
+    if constexpr (!AHEAD) {
+      int any = 0;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) any |= b.bad[w];
+      // A value of V that is not finite, times the zeros above the diagonal, would reach the tokens before it: such a
+      // block's weights and values are summed pair by pair.
+      if (__builtin_amdgcn_readfirstlane(any)) {
+        __syncthreads();                 // P is whole
+        for (int j = 0; j < kC; ++j) {
+          const bf16x4 x = *reinterpret_cast<const bf16x4*>(&b.v[j * VS + 16 * wave + 4 * g]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float w = float(pm[half][(16 * i + l16) * PS + j / 32 * 32 + j / 4 % 4 * 8 + j / 16 % 2 * 4 + j % 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][e] = j <= 16 * i + l16 ? fmaf(w, float(x[e]), o[i][e]) : o[i][e];
+          }
+        }
+        put(t0);
+        pending = false;
+      }
     }
+    if (BUF == 1) __syncthreads();
+    store(blk[(half ^ 1) % BUF], rows, t0 + kC);
+    load(rows, t0 + 2 * kC);
     __syncthreads();
   }
-  if (!AHEAD) {
+  if (pending) {
     const int blocks = (it.len + kC - 1) / kC;
-    finish(blk[(blocks - 1) & 1], (blocks - 1) * kC);
+    finish(pm[(blocks - 1) & 1], (blocks - 1) * kC);
   }
 
   const int64_t size = int64_t(DK) * DV;
@@ -392,7 +428,7 @@ __global__ __launch_bounds__(256) void lin_step_kernel(LinDevPlan p, const __bf1
   __shared__ __attribute__((aligned(16))) f32x4 sum[RG][W / 4];
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
-  const LinItem it = p.steps[blockIdx.x / (DV / W) / H];
+  const LinItem it = item_at(p.steps + blockIdx.x / (DV / W) / H);
   const int head = blockIdx.x / (DV / W) % H, c0 = blockIdx.x % (DV / W) * W, qk_head = head / (H / Hqk);
   const int tid = threadIdx.x, cq = tid % (W / 4), rg = tid / (W / 4), at = c0 + 4 * cq;
   const int64_t size = int64_t(DK) * DV;

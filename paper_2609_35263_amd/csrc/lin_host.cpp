@@ -64,7 +64,7 @@ int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wave
   if (!std::isfinite(s.scale)) return set_error(WAVEPP_EINVAL, "scale must be finite");
   if ((s.head_dim_k != 64 && s.head_dim_k != 128) || (s.head_dim_v != 64 && s.head_dim_v != 128))
     return set_error(WAVEPP_EUNSUPPORTED, "unsupported head dims (d_k=%d, d_v=%d): each 64 or 128", s.head_dim_k, s.head_dim_v);
-  if (int64_t(s.num_heads) * 128 > INT32_MAX / 4) return set_error(WAVEPP_EINVAL, "too many heads");
+  if (s.num_heads > 65535) return set_error(WAVEPP_EINVAL, "too many heads");   // a block of rows stays within 32-bit offsets
   const int32_t R = batch->num_requests;
   if (R < 0) return set_error(WAVEPP_EINVAL, "num_requests < 0");
   if (R > 0 && (!batch->chunk_lens || !batch->state_in || !batch->state_out))
