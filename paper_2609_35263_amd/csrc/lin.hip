@@ -282,16 +282,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
   bool pending = false;
   for (int t0 = 0, half = 0; t0 < it.len; t0 += kC, half ^= 1) {
     const Block& b = blk[half % BUF];
-    if (pending) finish(pm[half ^ 1], t0 - kC);
     if constexpr (!AHEAD) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = f32x4{};
-#pragma unroll
-      for (int s = 0; s < CT / 2; ++s) {
-        const bf16x8 st = acc_operand(S[2 * s], S[2 * s + 1]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = mfma(st, operand(b.q, (16 * i + l16) * QS + 32 * s + 8 * g), o[i]);
-      }
       for (int tile = wave; tile < 10; tile += NW) {       // (queries ti, keys tj), ti >= tj
         const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
         f32x4 x = f32x4{};                                 // K Q^T: keys 4 g .. + 3 of query l16
@@ -314,6 +305,17 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
           for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
         }
         *reinterpret_cast<bf16x4*>(&pm[half][(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
+      }
+    }
+    if (pending) finish(pm[half ^ 1], t0 - kC);
+    if constexpr (!AHEAD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = f32x4{};
+#pragma unroll
+      for (int s = 0; s < CT / 2; ++s) {
+        const bf16x8 st = acc_operand(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = mfma(st, operand(b.q, (16 * i + l16) * QS + 32 * s + 8 * g), o[i]);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
