@@ -134,8 +134,11 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
-  const LinItem it = item_at(p.segments + blockIdx.x / H);
-  const int head = blockIdx.x % H, qk_head = head / (H / Hqk);
+  // Workgroups go round-robin to the kNumXcd L2 domains: the heads that share a q/k head read its rows through one.
+  const int G = H / Hqk, unit = blockIdx.x / (kNumXcd * G) * kNumXcd + blockIdx.x % kNumXcd;
+  if (unit >= (AHEAD ? p.num_ahead : p.num_segments) * Hqk) return;
+  const LinItem it = item_at(p.segments + unit / Hqk);
+  const int qk_head = unit % Hqk, head = qk_head * G + blockIdx.x / kNumXcd % G;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -479,16 +482,20 @@ template <int DK, int DV>
 hipError_t launch_dims(const LinDevPlan& p, const __bf16* q, const __bf16* k, const __bf16* v, const float* alpha,
                        float* pool, __bf16* out, hipStream_t stream) {
   const int H = p.num_heads;
+  // a workgroup for every (segment, head), the segments' q/k heads padded to whole rounds of the L2 domains
+  auto grid = [&](int segments) {
+    return dim3((segments * p.num_qk_heads + kNumXcd - 1) / kNumXcd * kNumXcd * (H / p.num_qk_heads));
+  };
   if (p.num_steps)
     hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(p.num_steps * H * (DV / 32)), dim3(256), 0, stream, p, q, k, v, alpha,
                        pool, out);
   if (p.num_ahead)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, true>), dim3(p.num_ahead * H), dim3(4 * DV), 0, stream, p, q, k, v, alpha,
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, true>), grid(p.num_ahead), dim3(4 * DV), 0, stream, p, q, k, v, alpha,
                        pool, out);
   if (p.num_scans)
     hipLaunchKernelGGL(lin_scan_kernel, dim3(p.num_scans * H, DK * DV / 1024), dim3(256), 0, stream, p, pool);
   if (p.num_segments)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, false>), dim3(p.num_segments * H), dim3(4 * DV), 0, stream, p, q, k, v,
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, false>), grid(p.num_segments), dim3(4 * DV), 0, stream, p, q, k, v,
                        alpha, pool, out);
   return hipGetLastError();
 }

@@ -11,8 +11,10 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <functional>
 #include <memory>
 #include <new>
+#include <queue>
 #include <vector>
 
 using namespace wavepp;
@@ -33,6 +35,14 @@ namespace {
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Constants of the model below, in blocks of the main kernel (about 3.5 us): what a workgroup takes besides its blocks in
+// either kernel, a block of the kernel that runs ahead, the scan's launch and one of its states of 128 x 128, and the
+// memory's time for a block of 128 + 128 columns.  Measured over forced cuts of seven waves (us, forced best / chosen):
+// 32 heads of 128 x 64, 4,627 + 4,948 + 6,968 tokens: 390 whole, 128 / 128; 64 of 128 x 128, 16,384 tokens: 912 whole,
+// 380 / 380; 16 of 64 x 64, 2 x 8,000: 329 whole, 55 / 55; 8 of 128 x 128, 16,384: 798 whole, 70 / 70.
+constexpr double kMainOverhead = 3.0, kAheadOverhead = 2.0, kAheadBlock = 0.5, kScanBase = 1.5, kScanBlock = 0.01;
+constexpr double kMemoryBlock = 0.0046;
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 int check_ws(const wavepp_lin_plan_t* plan, void* ws, size_t ws_bytes) {
@@ -43,12 +53,74 @@ int check_ws(const wavepp_lin_plan_t* plan, void* ws, size_t ws_bytes) {
   return WAVEPP_OK;
 }
 
-// Blocks per segment: enough segments to fill the chip's 512 resident workgroups where the chains alone do not.
-int64_t segment_blocks(const std::vector<int64_t>& blocks, int heads) {
-  int64_t total = 0, longest = 1;
-  for (int64_t b : blocks) total += b, longest = std::max(longest, b);
-  if (int64_t(blocks.size()) * heads >= kNumCu) return longest;
-  return std::max<int64_t>(4, ceil_div(total * heads, 2 * kNumCu));
+// How a chunk of n blocks is cut into at most `pieces` segments of equal length, the last shorter: blocks of one, their number.
+struct Cut {
+  int64_t each, count;
+  Cut(int64_t n, int64_t pieces) : each(ceil_div(n, std::max<int64_t>(1, std::min(n, pieces)))), count(ceil_div(n, each)) {}
+};
+
+// The time at which the last of `runs` (length, how many) ends, longest first on `slots` workgroups that run one
+// after another; every one takes `overhead` besides its length.
+double makespan(std::vector<std::pair<int64_t, int64_t>> runs, int64_t slots, double overhead) {
+  std::sort(runs.rbegin(), runs.rend());
+  std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
+  double longest = 0.0;
+  for (const auto& r : runs)
+    for (int64_t i = 0; i < r.second; ++i) {
+      double t = double(r.first) + overhead;
+      if (int64_t(busy.size()) == slots) {
+        t += busy.top();
+        busy.pop();
+      }
+      busy.push(t);
+      longest = std::max(longest, t);
+    }
+  return longest;
+}
+
+// Modelled time, in blocks of the main kernel, of chunks of `blocks` (one for each of `heads` chains), cut so that
+// no segment is longer than `most`; some number no less than `best` where it cannot beat that.
+double cut_cost(const wavepp_lin_shape& s, const std::vector<int64_t>& blocks, int64_t most, double best) {
+  const int64_t slots = kNumCu * (s.head_dim_v == 64 ? 2 : 1), H = s.num_heads;
+  // what memory takes for a block: rows of q, k, v and out in the main kernel, of k and v in the one that runs ahead; heads
+  // that share q and k read them from one L2
+  const double traffic = kMemoryBlock * (double(s.head_dim_k) * s.num_qk_heads / s.num_heads + s.head_dim_v) / 256.0;
+  std::vector<std::pair<int64_t, int64_t>> all, ahead;
+  int64_t parts = 0, total = 0, early = 0, count = 0;
+  for (int64_t n : blocks) {
+    const Cut c(n, ceil_div(n, most));
+    total += n * H;
+    count += c.count * H;
+    all.push_back({n - c.each * (c.count - 1), H});
+    if (c.count == 1) continue;
+    all.push_back({c.each, (c.count - 1) * H});
+    ahead.push_back({c.each, (c.count - 1) * H});
+    early += c.each * (c.count - 1) * H;
+    parts += c.count - 1;
+  }
+  const double scan = parts ? kScanBase + kScanBlock * double(parts) * H * (s.head_dim_k * s.head_dim_v / 16384.0) : 0.0;
+  const double bound = std::max((double(total) + kMainOverhead * double(count)) / double(slots), traffic * double(total)) + scan;
+  if (bound >= best) return bound;
+  double t = scan + std::max(makespan(std::move(all), slots, kMainOverhead), traffic * double(total));
+  if (parts)
+    t += std::max(kAheadBlock * makespan(std::move(ahead), 2 * kNumCu, kAheadOverhead), 0.5 * traffic * double(early));
+  return t;
+}
+
+// The longest segment, in blocks: a chunk whole where the chains fill the chip, else what cut_cost likes best.
+int64_t segment_blocks(const wavepp_lin_shape& s, const std::vector<int64_t>& blocks) {
+  const int64_t longest = *std::max_element(blocks.begin(), blocks.end());
+  if (int64_t(blocks.size()) * s.num_heads >= 4 * kNumCu) return longest;
+  int64_t best = longest;
+  double least = cut_cost(s, blocks, longest, INFINITY);
+  for (int64_t pieces = 2, last = longest; pieces <= 2 * kNumCu && last > 2; ++pieces) {
+    const int64_t most = ceil_div(longest, pieces);
+    if (most == last) continue;
+    last = most;
+    const double t = cut_cost(s, blocks, most, least);
+    if (t < least) least = t, best = most;
+  }
+  return best;
 }
 
 int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wavepp_lin_plan_t** out) {
@@ -102,7 +174,7 @@ int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wave
   std::vector<int64_t> blocks;
   for (int32_t r = 0; r < R; ++r)
     if (batch->chunk_lens[r] > kLinStepTokens) blocks.push_back(ceil_div(batch->chunk_lens[r], kLinBlock));
-  const int64_t per = blocks.empty() ? 1 : segment_blocks(blocks, s.num_heads);
+  const int64_t per = blocks.empty() ? 1 : segment_blocks(s, blocks);
   std::vector<LinItem> last;            // segments without a partial state of their own
   int64_t cu = 0, parts = 0;
   for (int32_t r = 0; r < R; ++r) {
@@ -119,8 +191,9 @@ int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wave
       plan->steps.push_back(it);
       continue;
     }
-    const int64_t n = ceil_div(c, kLinBlock), pieces = ceil_div(n, per), each = ceil_div(n, pieces);
-    const int64_t count = ceil_div(n, each);
+    const int64_t n = ceil_div(c, kLinBlock);
+    const Cut cut(n, ceil_div(n, per));
+    const int64_t each = cut.each, count = cut.count;
     // the last segment may end before the first has read its start, so a slot that is resumed in place is copied first
     const bool copied = count > 1 && it.state_in >= 0 && it.state_in == it.state_out;
     const int32_t start = copied ? int32_t(parts + count - 1) : -1;
