@@ -383,6 +383,40 @@ struct SplitPlan {
   int64_t pieces = 0;
 };
 
+// The cut of a wave of few rows over 4-bit pages, which streams the cache on `slots` workgroups.  Pieces of the mean load
+// of a slot (at least `least` tiles) fill the chip once where that comes out even.  Where it does not -- nearly as many
+// items as slots, or more, of unlike lengths -- the longest would run on after the others with the memory
+// half idle, so no piece is longer than half the mean load then.  64 requests of 1-32 K cached tokens, 8 KV heads of
+// 128: 255 us whole, 229 cut so (233 and 237 with pieces half and a third as long); 128 of 16-4,000 tokens, 4 of 64: 29 and
+// 26; 8 of 32,000, 8 heads: 62 once, 65 cut so.
+SplitPlan few_rows_split(const std::vector<int64_t>& ntiles, int64_t slots, int64_t least) {
+  int64_t longest = 1, total = 0;
+  for (int64_t t : ntiles) {
+    longest = std::max(longest, t);
+    total += t;
+  }
+  auto count = [&](int64_t T) {
+    int64_t n = 0;
+    for (int64_t t : ntiles) n += ceil_div(t, T);
+    return n;
+  };
+  // the shortest pieces of which there are no more than slots (the number of them does not grow with their length)
+  int64_t lo = std::max<int64_t>(1, least) - 1, hi = std::max(lo + 1, longest);
+  while (hi - lo > 1) {
+    const int64_t mid = lo + (hi - lo) / 2;
+    if (count(mid) <= slots) hi = mid; else lo = mid;
+  }
+  int64_t T = hi;
+  if (5 * T * slots > 7 * total) T = std::min(T, std::max(least, (total + slots) / (2 * slots)));
+  SplitPlan sp;
+  sp.tps.reserve(ntiles.size());
+  for (int64_t t : ntiles) {
+    sp.tps.push_back(ceil_div(t, ceil_div(t, T)));
+    sp.pieces += ceil_div(t, sp.tps.back());
+  }
+  return sp;
+}
+
 // Modelled time of a wave of pieces, in tiles, each costing its tiles plus `overhead` (queries in, partial out);
 // every piece of a split item adds its partial rows to the merge.  The pieces are handed out longest first
 // (Dispatch).  Played as one queue in front of 256 CUs, whole pieces with remainders that fit between them look 5-20 %
@@ -768,6 +802,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   SplitPlan split{ntiles, int64_t(base.size())};
   if (max_splits >= 1) {
     for (size_t i = 0; i < base.size(); ++i) split.tps[i] = ceil_div(ntiles[i], std::min<int64_t>(max_splits, ntiles[i]));
+  } else if (few_rows) {
+    split = few_rows_split(ntiles, fill_target, min_split_tiles);
   } else if (int64_t(base.size()) < fill_target) {
     auto auto_splits = [&](int64_t n, int64_t T) {       // (32-bit divisions: this runs a dozen times an item)
       return std::max<int64_t>(1, std::min(uint32_t(n + T - 1) / uint32_t(T), uint32_t(n) / uint32_t(min_split_tiles)));

@@ -35,6 +35,11 @@ __device__ __forceinline__ bf16x8 q4_values(uint32_t codes, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// Where the 8-value piece c of a V row lies in its LDS row (stride 16 banks past a multiple of 64): the four pieces of a
+// block of 32 exchange places by the block's number.  A thread writes one block piece by piece; in order, all threads'
+// pieces of one turn would fall on a quarter of the banks (192 of 290 LDS cycles a block of 32 keys were such conflicts).
+__device__ __forceinline__ int v_place(int c) { return 8 * (c ^ ((c >> 2) & 3)); }
+
 // ---------------------------------------------------------------------------------------------
 // Append and read.  One thread moves eight values of a row (16 bytes of bf16, 4 of codes); the four
 // threads of a block of 32 find its largest magnitude between them.  A workgroup takes TOK consecutive tokens.
@@ -209,12 +214,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
   };
   auto store_tile = [&](int buf) {
     __bf16* kd = &ks[buf][key * KSTR + part * (W * 8)];
-    __bf16* vd = &vs[buf][key * VSTR + part * (W * 8)];
     const float a = scale_of(kscale), b = scale_of(vscale);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       *reinterpret_cast<bf16x8*>(kd + 8 * i) = q4_values(kreg[i], a);
-      *reinterpret_cast<bf16x8*>(vd + 8 * i) = q4_values(vreg[i], b);
+      *reinterpret_cast<bf16x8*>(&vs[buf][key * VSTR + v_place(part * W + i)]) = q4_values(vreg[i], b);
     }
   };
 
@@ -222,7 +226,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
   // 16-wide step.  V (A operand of O^T = V^T P^T, read transposed): within its 16-lane group, lane
   // j = lane % 16 addresses key 4*hf + j/4 and d = 16*((lane/16) % 2) + 4*(j%4) of a 16-key step.
   const int k_lane = col * KSTR + 8 * hf;
-  const int v_lane = (4 * hf + (lane & 15) / 4) * VSTR + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  int v_lane[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+    v_lane[db] = (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 4 * (lane & 1);
 
   const int t_begin = it.kv_begin / KT;
   const int t_end = (it.kv_end + KT - 1) / KT;
@@ -307,13 +314,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
       m_run = m_new;
       // O^T[d][row] += V^T[d][key] P^T[key][row]; step t covers keys 16t + 8*(e/4) + 4*hf + (e%4),
       // the order in which the S^T accumulator holds them
-      const __bf16* vl = &vs[buf][v_lane];
+      const __bf16* vl = &vs[buf][0];
 #pragma unroll
       for (int t = 0; t < 2 * NKB; ++t)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          const bf16x4 lo = lds_read_tr(vl + 16 * t * VSTR + 32 * db);
-          const bf16x4 hi = lds_read_tr(vl + (16 * t + 8) * VSTR + 32 * db);
+          const bf16x4 lo = lds_read_tr(vl + v_lane[db] + 16 * t * VSTR);
+          const bf16x4 hi = lds_read_tr(vl + v_lane[db] + (16 * t + 8) * VSTR);
           const bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t], oacc[db], 0, 0, 0);
         }
@@ -443,7 +450,10 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
   };
 
   __bf16* const vs = reinterpret_cast<__bf16*>(smem + wave * VBYTES);
-  const __bf16* const vl = vs + (4 * hf + (lane & 15) / 4) * VSTR + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  const __bf16* vl[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+    vl[db] = vs + (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 4 * (lane & 1);
   f32x16 oacc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
@@ -464,9 +474,9 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
     for (int i = 0; i < NL; ++i) {
       const int piece = lane + 64 * i;
       const float a = scale_of(b.vscale[i]);
-      __bf16* row = vs + piece / NB * VSTR + 32 * (piece % NB);
+      __bf16* row = vs + piece / NB * VSTR;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) *reinterpret_cast<bf16x8*>(row + 8 * u) = q4_values(b.v[i][u], a);
+      for (int u = 0; u < 4; ++u) *reinterpret_cast<bf16x8*>(row + v_place(4 * (piece % NB) + u)) = q4_values(b.v[i][u], a);
     }
     // accumulator element r holds key 8*(r/4) + 4*hf + (r%4)
     if (kbase + 31 > min_lim || kbase + 32 > it.kv_end) {
@@ -505,23 +515,31 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) {
-        const bf16x4 lo = lds_read_tr(vl + 16 * t * VSTR + 32 * db);
-        const bf16x4 hi = lds_read_tr(vl + (16 * t + 8) * VSTR + 32 * db);
+        const bf16x4 lo = lds_read_tr(vl[db] + 16 * t * VSTR);
+        const bf16x4 hi = lds_read_tr(vl[db] + (16 * t + 8) * VSTR);
         const bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t], oacc[db], 0, 0, 0);
       }
   };
 
+  // Two blocks are in flight.  Loads are not branched around (a last block is loaded again instead), so the compiler
+  // knows their number and waits for the older block alone.
   const int end = (it.kv_end + 31) / 32;
   int block = it.kv_begin / 32 + wave;
-  Block b0, b1;
-  if (block < end) load(b0, block);
-  if (block + 4 < end) load(b1, block + 4);
-  for (; block < end; block += 8) {
-    attend(b0, block);
-    if (block + 8 < end) load(b0, block + 8);
-    if (block + 4 < end) attend(b1, block + 4);
-    if (block + 12 < end) load(b1, block + 12);
+  if (block < end) {
+    Block b0, b1;
+    load(b0, block);
+    __builtin_amdgcn_sched_barrier(0);
+    load(b1, min(block + 4, end - 1));
+    for (;;) {
+      attend(b0, block);
+      load(b0, min(block + 8, end - 1));
+      if (block + 4 >= end) break;
+      attend(b1, block + 4);
+      load(b1, min(block + 12, end - 1));
+      block += 8;
+      if (block >= end) break;
+    }
   }
 
   // ---- the waves' sums joined -------------------------------------------------------------------
