@@ -344,6 +344,18 @@ def _dtypes():
     return _bf16, _f32
 
 
+_types = None
+
+
+def _torch_types():
+    """(bfloat16, uint8, float32)."""
+    global _types
+    if _types is None:
+        import torch
+        _types = torch.bfloat16, torch.uint8, torch.float32
+    return _types
+
+
 def _stream(stream):
     if stream is None:
         import torch
@@ -351,18 +363,39 @@ def _stream(stream):
     return stream.cuda_stream
 
 
-def _stream_for(stream, *tensors):
-    """The stream of a call whose buffers all have to be on the current device, which is where it launches."""
+def _call_args(stream, *buffers):
+    """Device addresses of a call's buffers (name, tensor, shape or None for any, dtype or None for any), then the stream, for
+    a call that launches on the current device: every buffer is a contiguous tensor on it of that shape and type, and so is
+    the stream."""
     import torch
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    args = []
+    for name, t, shape, dtype in buffers:
+        if t is None or t.get_device() != here or (shape is not None and t.shape != shape) or \
+                (dtype is not None and t.dtype is not dtype) or not t.is_contiguous():
+            _refuse(buffers, here)
+        args.append(t.data_ptr())
     if stream is None:
-        stream = torch.cuda.current_stream()
-    here = torch.cuda.current_device()
-    if stream.device.index != here:
+        # the current stream's handle alone: a Stream object costs 2.5 us, a third of such a call
+        args.append(torch._C._cuda_getCurrentRawStream(here))
+    elif stream.device.index != here:
         raise ValueError(f"the stream is of {stream.device}, the current device is {here}")
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"a buffer is on {t.device}, the current device is {here}")
-    return stream.cuda_stream
+    else:
+        args.append(stream.cuda_stream)
+    return args
+
+
+def _refuse(buffers, here):
+    """Says what is wrong with the buffers of _call_args: what is missing, then shapes, then the rest."""
+    for name, t, _, _ in buffers:
+        if t is None:
+            raise ValueError(f"{name} is required")
+    _check_shapes(*((name, t, shape) for name, t, shape, _ in buffers if shape is not None))
+    for name, t, _, dtype in buffers:
+        _ptr(t, dtype, name)
+        if t.get_device() != here:
+            raise ValueError(f"{name} is on {t.device}, the current device is {here}")
+    raise ValueError("a buffer cannot be used")
 
 
 def _check_shapes(*named):
@@ -502,52 +535,37 @@ def _q4_shapes(p: Plan) -> dict:
     return sh
 
 
-def _required(**bufs):
-    for name, t in bufs.items():
-        if t is None:
-            raise ValueError(f"{name} is required")
-
-
 def q4_append_kv(p: Plan, k_new, v_new, k_pool, v_pool, workspace, stream=None):
     """Quantise the wave's new K/V rows into their pages."""
-    import torch
-    bf, _ = _dtypes()
+    bf, u8 = _torch_types()[:2]
     sh = _q4_shapes(p)
-    _required(k_new=k_new, v_new=v_new, k_pool=k_pool, v_pool=v_pool)
-    _check_shapes(("k_new", k_new, sh["k_new"]), ("v_new", v_new, sh["v_new"]), ("k_pool", k_pool, sh["pool"]),
-                  ("v_pool", v_pool, sh["pool"]))
-    _check(load_library().wavepp_q4_append_kv(
-        p.handle, _ptr(k_new, bf, "k_new"), _ptr(v_new, bf, "v_new"), _ptr(k_pool, torch.uint8, "k_pool"),
-        _ptr(v_pool, torch.uint8, "v_pool"), _ptr(workspace, name="workspace"), workspace.nbytes,
-        _stream_for(stream, k_new, v_new, k_pool, v_pool, workspace)))
+    k, v, kp, vp, ws, st = _call_args(stream, ("k_new", k_new, sh["k_new"], bf), ("v_new", v_new, sh["v_new"], bf),
+                                      ("k_pool", k_pool, sh["pool"], u8), ("v_pool", v_pool, sh["pool"], u8),
+                                      ("workspace", workspace, None, None))
+    _check(load_library().wavepp_q4_append_kv(p.handle, k, v, kp, vp, ws, workspace.nbytes, st))
 
 
 def q4_read_kv(p: Plan, k_pool, v_pool, k_out, v_out, workspace, stream=None):
     """The bf16 rows of the wave's new tokens as the pages hold them."""
-    import torch
-    bf, _ = _dtypes()
+    bf, u8 = _torch_types()[:2]
     sh = _q4_shapes(p)
-    _required(k_pool=k_pool, v_pool=v_pool, k_out=k_out, v_out=v_out)
-    _check_shapes(("k_pool", k_pool, sh["pool"]), ("v_pool", v_pool, sh["pool"]), ("k_out", k_out, sh["k_new"]),
-                  ("v_out", v_out, sh["v_new"]))
-    _check(load_library().wavepp_q4_read_kv(
-        p.handle, _ptr(k_pool, torch.uint8, "k_pool"), _ptr(v_pool, torch.uint8, "v_pool"), _ptr(k_out, bf, "k_out"),
-        _ptr(v_out, bf, "v_out"), _ptr(workspace, name="workspace"), workspace.nbytes,
-        _stream_for(stream, k_pool, v_pool, k_out, v_out, workspace)))
+    kp, vp, k, v, ws, st = _call_args(stream, ("k_pool", k_pool, sh["pool"], u8), ("v_pool", v_pool, sh["pool"], u8),
+                                      ("k_out", k_out, sh["k_new"], bf), ("v_out", v_out, sh["v_new"], bf),
+                                      ("workspace", workspace, None, None))
+    _check(load_library().wavepp_q4_read_kv(p.handle, kp, vp, k, v, ws, workspace.nbytes, st))
 
 
 def q4_chunked_prefill(p: Plan, q, k_pool, v_pool, out, lse, workspace, stream=None):
     """Attention of the wave's queries over 4-bit pages (lse may be None)."""
-    import torch
-    bf, f32 = _dtypes()
+    bf, u8, f32 = _torch_types()
     sh = _q4_shapes(p)
-    _required(q=q, k_pool=k_pool, v_pool=v_pool, out=out)
-    _check_shapes(("q", q, sh["q"]), ("k_pool", k_pool, sh["pool"]), ("v_pool", v_pool, sh["pool"]),
-                  ("out", out, sh["out"]), ("lse", lse, sh["lse"]))
-    _check(load_library().wavepp_q4_chunked_prefill(
-        p.handle, _ptr(q, bf, "q"), _ptr(k_pool, torch.uint8, "k_pool"), _ptr(v_pool, torch.uint8, "v_pool"),
-        _ptr(out, bf, "out"), _ptr(lse, f32, "lse"), _ptr(workspace, name="workspace"), workspace.nbytes,
-        _stream_for(stream, q, k_pool, v_pool, out, lse, workspace)))
+    bufs = [("q", q, sh["q"], bf), ("k_pool", k_pool, sh["pool"], u8), ("v_pool", v_pool, sh["pool"], u8),
+            ("out", out, sh["out"], bf), ("workspace", workspace, None, None)]
+    if lse is not None:
+        bufs.append(("lse", lse, sh["lse"], f32))
+    args = _call_args(stream, *bufs)
+    _check(load_library().wavepp_q4_chunked_prefill(p.handle, *args[:4], None if lse is None else args[5], args[4],
+                                                    workspace.nbytes, args[-1]))
 
 
 # ------------------------------------------------------------------------------------------------
@@ -699,21 +717,18 @@ def lin_plan(*, num_heads, num_qk_heads, head_dim_k, head_dim_v, num_state_slots
 
 
 def lin_upload(p: LinPlan, workspace, stream=None):
-    _check(load_library().wavepp_lin_upload(p.handle, _ptr(workspace, name="workspace"), workspace.nbytes,
-                                            _stream_for(stream, workspace)))
+    ws, st = _call_args(stream, ("workspace", workspace, None, None))
+    _check(load_library().wavepp_lin_upload(p.handle, ws, workspace.nbytes, st))
 
 
 def lin_chunked_prefill(p: LinPlan, q, k, v, alpha, state_pool, out, workspace, stream=None):
     """One layer of the wave: out and the snapshots named by state_out."""
-    bf, f32 = _dtypes()
+    bf, _, f32 = _torch_types()
     sh = p._buffers
-    _required(q=q, k=k, v=v, alpha=alpha, state_pool=state_pool, out=out)
-    _check_shapes(("q", q, sh["qk"]), ("k", k, sh["qk"]), ("v", v, sh["v"]), ("alpha", alpha, sh["alpha"]),
-                  ("state_pool", state_pool, sh["state_pool"]), ("out", out, sh["v"]))
-    _check(load_library().wavepp_lin_chunked_prefill(
-        p.handle, _ptr(q, bf, "q"), _ptr(k, bf, "k"), _ptr(v, bf, "v"), _ptr(alpha, f32, "alpha"),
-        _ptr(state_pool, f32, "state_pool"), _ptr(out, bf, "out"), _ptr(workspace, name="workspace"), workspace.nbytes,
-        _stream_for(stream, q, k, v, alpha, state_pool, out, workspace)))
+    *bufs, ws, st = _call_args(stream, ("q", q, sh["qk"], bf), ("k", k, sh["qk"], bf), ("v", v, sh["v"], bf),
+                               ("alpha", alpha, sh["alpha"], f32), ("state_pool", state_pool, sh["state_pool"], f32),
+                               ("out", out, sh["v"], bf), ("workspace", workspace, None, None))
+    _check(load_library().wavepp_lin_chunked_prefill(p.handle, *bufs, ws, workspace.nbytes, st))
 
 
 # ------------------------------------------------------------------------------------------------
