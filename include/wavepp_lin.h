@@ -17,7 +17,7 @@
  *   alpha     [T][num_heads] or [num_heads]   fp32
  *   state_pool[num_state_slots][num_heads][head_dim_k][head_dim_v]   fp32
  *
- * Numerics: the state is carried and stored in fp32.  Chunks of at most 16 tokens run token by token
+ * Numerics: the state is carried and stored in fp32.  Chunks of at most 10 tokens run token by token
  * in fp32; longer ones in blocks of 64 tokens on bf16 matrix instructions with fp32 accumulation, where the
  * decay-weighted values that enter the state are two bf16 parts each (2^-16 relative), and the
  * weights inside a block and the state as the block's queries read it are rounded to bf16 (2^-8).  Outputs

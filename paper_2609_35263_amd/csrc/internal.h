@@ -113,7 +113,9 @@ struct alignas(16) KdaItem {
 // ---------------------------------------------------------------------------------------------
 constexpr uint32_t kLinMagic = 0x4C494E31u;  // "LIN1"
 constexpr int kLinBlock = 64;                // tokens per block of the chunkwise form
-constexpr int kLinStepTokens = 16;           // chunks up to this length run token by token
+// Chunks up to this length run token by token: 64 requests of 64 heads of 128 x 128 take 128 us so and 154 in blocks at
+// eight tokens, 159 and 156 at twelve, 197 and 158 at sixteen; 4 of 32 of 128 x 64: 7.1 and 9.0, 8.9 and 9.2, 11.1 and 9.1.
+constexpr int kLinStepTokens = 10;
 
 struct alignas(16) LinHeader {
   uint32_t magic;

@@ -117,6 +117,9 @@ int64_t segment_blocks(const wavepp_lin_shape& s, const std::vector<int64_t>& bl
     const int64_t most = ceil_div(longest, pieces);
     if (most == last) continue;
     last = most;
+    int64_t count = 0;
+    for (int64_t n : blocks) count += Cut(n, ceil_div(n, most)).count;
+    if (count * s.num_heads > 8 * kNumCu) break;           // rounds enough for any unevenness
     const double t = cut_cost(s, blocks, most, least);
     if (t < least) least = t, best = most;
   }
@@ -226,7 +229,7 @@ int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wave
   std::stable_sort(plan->steps.begin(), plan->steps.end(), longer);
   plan->segments.insert(plan->segments.end(), last.begin(), last.end());
   const int64_t most = std::max({int64_t(plan->segments.size()), int64_t(plan->steps.size())});
-  if (most * s.num_heads > INT32_MAX / 64) return set_error(WAVEPP_EINVAL, "too many workgroups");
+  if (most * s.num_heads >= 1 << 22) return set_error(WAVEPP_EINVAL, "too many workgroups");   // 2^32 threads a launch
 
   plan->off_steps = sizeof(LinHeader);
   plan->off_segments = plan->off_steps + sizeof(LinItem) * plan->steps.size();

@@ -45,6 +45,12 @@ __device__ __forceinline__ int v_place(int c) { return 8 * (c ^ ((c >> 2) & 3));
 // threads of a block of 32 find its largest magnitude between them.  A workgroup takes TOK consecutive tokens.
 // ---------------------------------------------------------------------------------------------
 
+// The value of another lane of the same four, by a quad permutation.
+template <int CTRL>
+__device__ __forceinline__ uint32_t quad_other(uint32_t x) {
+  return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, true));
+}
+
 // The request that holds packed token t: the last with cu <= t (requests without a chunk share cu with the next).
 __device__ __forceinline__ int request_of(const DevPlan& p, int64_t t) {
   int lo = 0, hi = p.num_requests - 1;
@@ -55,19 +61,29 @@ __device__ __forceinline__ int request_of(const DevPlan& p, int64_t t) {
   return lo;
 }
 
-// Calls move(token, page of the pool, slot in it) for the workgroup's tokens.
-template <int TOK, class Move>
-__device__ __forceinline__ void each_token(const DevPlan& p, Move move) {
-  const int64_t t0 = int64_t(blockIdx.x) * TOK;
+// The first of the workgroup's TOK tokens.  Each L2 domain (workgroups go to them round-robin) has a run of the wave's
+// tokens, so that the rows and scales that share a line of a page meet in one L2.
+template <int TOK>
+__device__ __forceinline__ int64_t first_token(const DevPlan& p) {
+  const int64_t per = gridDim.x / kNumXcd;
+  return (int64_t(blockIdx.x) % kNumXcd * per + blockIdx.x / kNumXcd) * TOK;
+}
+
+// The workgroup's tokens: page of the pool and slot in it of each; the number of tokens.
+template <int TOK>
+__device__ __forceinline__ int token_places(const DevPlan& p, int64_t t0, int64_t (&page)[TOK], int (&slot)[TOK]) {
   int r = request_of(p, t0);
-  for (int i = 0; i < TOK && t0 + i < p.total_tokens; ++i) {
-    const int64_t t = t0 + i;
+  const int n = int(min(int64_t(TOK), p.total_tokens - t0));
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    const int64_t t = t0 + min(i, n - 1);
     while (r + 1 < p.num_requests && const_load(&p.reqs[r + 1].cu) <= t) ++r;
     const ReqMeta* rq = &p.reqs[r];
     const int pos = const_load(&rq->prefix) + int(t - const_load(&rq->cu));
-    const int64_t page = const_load(&p.bt[const_load(&rq->bt_row) + pos / p.page_size]);
-    move(t, page, pos % p.page_size);
+    page[i] = const_load(&p.bt[const_load(&rq->bt_row) + pos / p.page_size]);
+    slot[i] = pos % p.page_size;
   }
+  return n;
 }
 
 template <int D, int TOK>
@@ -77,22 +93,31 @@ __global__ __launch_bounds__(256) void q4_append_kernel(DevPlan p, const u32x4* 
   if (!meta_ok(p)) return;
   constexpr int CH = D / 8, NB = D / kQ4Block;
   const int Hkv = p.num_kv_heads, B = p.page_size;
-  const int64_t page_bytes = int64_t(B) * (D / 2 + NB);
-  each_token<TOK>(p, [&](int64_t t, int64_t page, int slot) {
-    for (int u = threadIdx.x; u < Hkv * 2 * CH; u += blockDim.x) {
-      const int h = u / (2 * CH), c = u % CH;
-      const bool is_v = u % (2 * CH) >= CH;
-      const u32x4 x = (is_v ? v_new : k_new)[(t * Hkv + h) * CH + c];
+  const int64_t page_bytes = int64_t(B) * (D / 2 + NB), t0 = first_token<TOK>(p);
+  if (t0 >= p.total_tokens) return;
+  int64_t page[TOK];
+  int slot[TOK];
+  const int n = token_places(p, t0, page, slot);
+  for (int u = threadIdx.x; u < Hkv * 2 * CH; u += blockDim.x) {
+    const int h = u / (2 * CH), c = u % CH;
+    const bool is_v = u % (2 * CH) >= CH;
+    const u32x4* rows = (is_v ? v_new : k_new) + (t0 * Hkv + h) * CH + c;
+    u32x4 x[TOK];
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) x[i] = rows[int64_t(min(i, n - 1)) * Hkv * CH];
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+      if (i >= n) break;
       // magnitudes of bf16 order like integers; NaN and infinities become the largest finite one
       uint32_t y[4], top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = min(x[i] & 0x7FFFu, 0x7F7Fu), hi = min((x[i] >> 16) & 0x7FFFu, 0x7F7Fu);
-        y[i] = (x[i] & 0x80008000u) | lo | (hi << 16);
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t lo = min(x[i][w] & 0x7FFFu, 0x7F7Fu), hi = min((x[i][w] >> 16) & 0x7FFFu, 0x7F7Fu);
+        y[w] = (x[i][w] & 0x80008000u) | lo | (hi << 16);
         top = max(top, max(lo, hi));
       }
-      top = max(top, uint32_t(__shfl_xor(int(top), 1)));
-      top = max(top, uint32_t(__shfl_xor(int(top), 2)));
+      top = max(top, quad_other<0xB1>(top));               // lanes 1, 0, 3, 2
+      top = max(top, quad_other<0x4E>(top));               // lanes 2, 3, 0, 1
       // top = 1.m * 2^(E - 127): the smallest s with top <= 7 s is 2^(E - 127 - 2), twice that where 1.m > 1.75
       const int e = min(max(int(top >> 7) - 2 + int((top & 0x7Fu) > 0x60u), 8), 252);
       const float s = scale_of(uint32_t(e));
@@ -101,11 +126,11 @@ __global__ __launch_bounds__(256) void q4_append_kernel(DevPlan p, const u32x4* 
       codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, y[1]), s, 1);
       codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, y[2]), s, 2);
       codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(codes, __builtin_bit_cast(bf16x2, y[3]), s, 3);
-      uint8_t* run = (is_v ? v_pool : k_pool) + (page * Hkv + h) * page_bytes;
-      *reinterpret_cast<uint32_t*>(run + slot * (D / 2) + 4 * c) = codes;
-      if (c % 4 == 0) run[B * (D / 2) + slot * NB + c / 4] = uint8_t(e);
+      uint8_t* run = (is_v ? v_pool : k_pool) + (page[i] * Hkv + h) * page_bytes;
+      *reinterpret_cast<uint32_t*>(run + slot[i] * (D / 2) + 4 * c) = codes;
+      if (c % 4 == 0) run[B * (D / 2) + slot[i] * NB + c / 4] = uint8_t(e);
     }
-  });
+  }
 }
 
 template <int D, int TOK>
@@ -115,16 +140,27 @@ __global__ __launch_bounds__(256) void q4_read_kernel(DevPlan p, const uint8_t* 
   if (!meta_ok(p)) return;
   constexpr int CH = D / 8, NB = D / kQ4Block;
   const int Hkv = p.num_kv_heads, B = p.page_size;
-  const int64_t page_bytes = int64_t(B) * (D / 2 + NB);
-  each_token<TOK>(p, [&](int64_t t, int64_t page, int slot) {
-    for (int u = threadIdx.x; u < Hkv * 2 * CH; u += blockDim.x) {
-      const int h = u / (2 * CH), c = u % CH;
-      const bool is_v = u % (2 * CH) >= CH;
-      const uint8_t* run = (is_v ? v_pool : k_pool) + (page * Hkv + h) * page_bytes;
-      const uint32_t codes = *reinterpret_cast<const uint32_t*>(run + slot * (D / 2) + 4 * c);
-      (is_v ? v_out : k_out)[(t * Hkv + h) * CH + c] = q4_values(codes, scale_of(run[B * (D / 2) + slot * NB + c / 4]));
+  const int64_t page_bytes = int64_t(B) * (D / 2 + NB), t0 = first_token<TOK>(p);
+  if (t0 >= p.total_tokens) return;
+  int64_t page[TOK];
+  int slot[TOK];
+  const int n = token_places(p, t0, page, slot);
+  for (int u = threadIdx.x; u < Hkv * 2 * CH; u += blockDim.x) {
+    const int h = u / (2 * CH), c = u % CH;
+    const bool is_v = u % (2 * CH) >= CH;
+    const uint8_t* pool = (is_v ? v_pool : k_pool) + h * page_bytes;
+    uint32_t codes[TOK], scale[TOK];
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+      const uint8_t* run = pool + page[i] * Hkv * page_bytes;
+      codes[i] = *reinterpret_cast<const uint32_t*>(run + slot[i] * (D / 2) + 4 * c);
+      scale[i] = run[B * (D / 2) + slot[i] * NB + c / 4];
     }
-  });
+    bf16x8* rows = (is_v ? v_out : k_out) + (t0 * Hkv + h) * CH + c;
+#pragma unroll
+    for (int i = 0; i < TOK; ++i)
+      if (i < n) rows[int64_t(i) * Hkv * CH] = q4_values(codes[i], scale_of(scale[i]));
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -603,6 +639,19 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
   }
 }
 
+// Launch shape of the append and the read: a token per workgroup in waves that do not fill the chip, four beyond, whose
+// rows are all loaded first (16,384 tokens of 8 heads of 128, stored and read back from cold memory: 49 us one by one, 44 with
+// two, 43 with four, 47 with eight).
+struct Moves {
+  bool few;
+  int64_t blocks;
+  int threads;
+  explicit Moves(const DevPlan& p)
+      : few(p.total_tokens <= 2048),
+        blocks(((few ? p.total_tokens : (p.total_tokens + 3) / 4) + kNumXcd - 1) / kNumXcd * kNumXcd),
+        threads(std::min(256, (p.num_kv_heads * p.head_dim_qk / 4 + 63) / 64 * 64)) {}
+};
+
 }  // namespace
 
 // ---------------------------------------------------------------------------------------------
@@ -610,16 +659,15 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
 // ---------------------------------------------------------------------------------------------
 hipError_t launch_q4_append(const DevPlan& p, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                             hipStream_t stream) {
-  const bool few = p.total_tokens <= 2048;
-  const int64_t blocks = few ? p.total_tokens : (p.total_tokens + 7) / 8;
-  const int threads = std::min(256, (p.num_kv_heads * p.head_dim_qk / 4 + 63) / 64 * 64);
+  const Moves g(p);
+  if (g.blocks >= 1 << 24) return hipErrorInvalidValue;
   auto kn = static_cast<const u32x4*>(k_new);
   auto vn = static_cast<const u32x4*>(v_new);
   auto kp = static_cast<uint8_t*>(k_pool);
   auto vp = static_cast<uint8_t*>(v_pool);
 #define WAVEPP_Q4_MOVE(D_)                                                                                            \
-  if (few) hipLaunchKernelGGL((q4_append_kernel<D_, 1>), dim3(blocks), dim3(threads), 0, stream, p, kn, vn, kp, vp);  \
-  else hipLaunchKernelGGL((q4_append_kernel<D_, 8>), dim3(blocks), dim3(threads), 0, stream, p, kn, vn, kp, vp);
+  if (g.few) hipLaunchKernelGGL((q4_append_kernel<D_, 1>), dim3(g.blocks), dim3(g.threads), 0, stream, p, kn, vn, kp, vp);  \
+  else hipLaunchKernelGGL((q4_append_kernel<D_, 4>), dim3(g.blocks), dim3(g.threads), 0, stream, p, kn, vn, kp, vp);
   if (p.head_dim_qk == 128) {
     WAVEPP_Q4_MOVE(128)
   } else if (p.head_dim_qk == 64) {
@@ -633,16 +681,15 @@ hipError_t launch_q4_append(const DevPlan& p, const void* k_new, const void* v_n
 
 hipError_t launch_q4_read(const DevPlan& p, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                           hipStream_t stream) {
-  const bool few = p.total_tokens <= 2048;
-  const int64_t blocks = few ? p.total_tokens : (p.total_tokens + 7) / 8;
-  const int threads = std::min(256, (p.num_kv_heads * p.head_dim_qk / 4 + 63) / 64 * 64);
+  const Moves g(p);
+  if (g.blocks >= 1 << 24) return hipErrorInvalidValue;
   auto kp = static_cast<const uint8_t*>(k_pool);
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto ko = static_cast<bf16x8*>(k_out);
   auto vo = static_cast<bf16x8*>(v_out);
 #define WAVEPP_Q4_MOVE(D_)                                                                                          \
-  if (few) hipLaunchKernelGGL((q4_read_kernel<D_, 1>), dim3(blocks), dim3(threads), 0, stream, p, kp, vp, ko, vo);  \
-  else hipLaunchKernelGGL((q4_read_kernel<D_, 8>), dim3(blocks), dim3(threads), 0, stream, p, kp, vp, ko, vo);
+  if (g.few) hipLaunchKernelGGL((q4_read_kernel<D_, 1>), dim3(g.blocks), dim3(g.threads), 0, stream, p, kp, vp, ko, vo);  \
+  else hipLaunchKernelGGL((q4_read_kernel<D_, 4>), dim3(g.blocks), dim3(g.threads), 0, stream, p, kp, vp, ko, vo);
   if (p.head_dim_qk == 128) {
     WAVEPP_Q4_MOVE(128)
   } else if (p.head_dim_qk == 64) {

@@ -71,7 +71,7 @@ def check(args, t, g, what="", finite=None):
     o, pool = oracle.lin.chunked_prefill(*ref)
     size, psize = oracle.lin.sizes(*ref)
     lens = np.asarray(args["chunk_lens"])
-    blocks = np.repeat(lens > 16, lens)[:, None, None]
+    blocks = np.repeat(lens > 10, lens)[:, None, None]
     bound = np.where(blocks, 1.1 * 2.0 ** -7, 1.02 * 2.0 ** -8) * size + 1e-30
     err = np.abs(g["out"].float().cpu().numpy().astype(np.float64) - o)
     assert (err <= bound).all(), (what, (err / bound).max())
@@ -80,7 +80,7 @@ def check(args, t, g, what="", finite=None):
     written = {int(s): int(c) for s, c in zip(args["state_out"], lens) if c}
     for s in range(got.shape[0]):
         if s in written:
-            b = (2.0 ** -14 if written[s] > 16 else 2.0 ** -18) * psize[s] + 1e-30
+            b = (2.0 ** -14 if written[s] > 10 else 2.0 ** -18) * psize[s] + 1e-30
             e = np.abs(got[s].numpy().astype(np.float64) - pool[s])
             assert (e <= b).all(), (what, s, (e / b).max())
             worst = max(worst, (e / b).max())
@@ -93,7 +93,7 @@ def check(args, t, g, what="", finite=None):
 @pytest.mark.parametrize("H,Hqk", [(4, 4), (6, 2), (5, 1)])
 @pytest.mark.parametrize("per_token", [True, False])
 def test_chunks_of_all_lengths(dk, dv, H, Hqk, per_token):
-    lens = [1, 63, 0, 64, 65, 2, 16, 17, 130, 200, 1]
+    lens = [1, 63, 0, 64, 65, 2, 10, 11, 130, 200, 1]
     s_in = [0, -1, 3, 1, 2, 3, -1, 4, 5, -1, 6]
     s_out = [0, 7, 3, 1, 8, 3, 9, 10, 11, 12, 6]
     args, t = make(lens, s_in, s_out, H, Hqk, dk, dv, seed=41, per_token=per_token, slots=14)
@@ -155,15 +155,15 @@ def test_chunk_by_chunk_and_token_by_token_equal_one_run():
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
 @pytest.mark.parametrize("name", ["q", "k", "v", "alpha"])
 def test_tokens_before_a_bad_number_are_as_without_it(name, bad):
-    lens = [200, 12, 90]
+    lens = [200, 9, 90]
     args, t = make(lens, [-1, 0, 1], [2, 3, 1], 3, 3, 128, 64, seed=47)
     a = on_gpu(args, t)
     spoiled = {n: x.clone() for n, x in t.items()}
-    for at in (75, 203, 300):                       # in the second block, in a token-by-token chunk, in a last block
+    for at in (75, 203, 290):                       # in the second block, in a token-by-token chunk, in a last block
         spoiled[name][at] = bad
     b = on_gpu(args, spoiled)
     clean = np.ones(sum(lens), dtype=bool)
-    for lo, hi in ((75, 76 if name == "q" else 200), (203, 204 if name == "q" else 212), (300, 301 if name == "q" else 302)):
+    for lo, hi in ((75, 76 if name == "q" else 200), (203, 204 if name == "q" else 209), (290, 291 if name == "q" else 299)):
         clean[lo:hi] = False
     x, y = (g["out"].float().cpu().numpy()[clean] for g in (a, b))
     assert np.isfinite(y).all()
@@ -171,7 +171,7 @@ def test_tokens_before_a_bad_number_are_as_without_it(name, bad):
                                                          args["state_out"], args["scale"]]
     size = oracle.lin.sizes(*ref)[0][clean]
     assert (np.abs(x - y) <= 2.2 * 2.0 ** -7 * size).all()
-    gone = b["out"].float().cpu().numpy()[[75, 203, 300]]
+    gone = b["out"].float().cpu().numpy()[[75, 203, 290]]
     assert not np.isfinite(gone).any()
 
 

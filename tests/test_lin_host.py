@@ -17,7 +17,7 @@ def kw(**over):
 
 
 @pytest.mark.parametrize("over,status", [
-    (dict(num_heads=0), -1), (dict(num_qk_heads=3), -1), (dict(num_qk_heads=16), -1), (dict(scale=float("nan")), -1),
+    (dict(num_heads=0), -1), (dict(num_heads=65536, num_qk_heads=1), -1), (dict(num_qk_heads=3), -1), (dict(num_qk_heads=16), -1), (dict(scale=float("nan")), -1),
     (dict(scale=float("inf")), -1), (dict(chunk_lens=[1, 0, -1]), -1), (dict(head_dim_k=96), -2), (dict(head_dim_v=256), -2),
     (dict(state_in=[6, 0, -1]), -3), (dict(state_in=[-2, 0, -1]), -3), (dict(state_out=[0, 0, 6]), -3),
     (dict(state_out=[-1, 0, 2]), -3), (dict(state_out=[2, 0, 2]), -4), (dict(state_in=[2, 0, -1]), -4),
@@ -33,7 +33,7 @@ def test_plan_of_both_forms():
     i = wp.lin_plan(**kw()).info()
     assert (i["total_tokens"], i["num_step_items"], i["num_segments"], i["num_partials"]) == (71, 1, 1, 0)
     assert wp.lin_plan(**kw(chunk_lens=[0, 0, 0])).info()["total_tokens"] == 0
-    assert wp.lin_plan(**kw(chunk_lens=[16, 0, 17])).info()["num_step_items"] == 1
+    assert wp.lin_plan(**kw(chunk_lens=[10, 0, 11])).info()["num_step_items"] == 1
     assert wp.lin_plan(**kw(chunk_lens=[], state_in=[], state_out=[])).info()["num_segments"] == 0
 
 
