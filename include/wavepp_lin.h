@@ -18,10 +18,11 @@
  *   state_pool[num_state_slots][num_heads][head_dim_k][head_dim_v]   fp32
  *
  * Numerics: the state is carried and stored in fp32.  Chunks of at most 10 tokens run token by token
- * in fp32; longer ones in blocks of 64 tokens on bf16 matrix instructions with fp32 accumulation, where the
- * decay-weighted values that enter the state are two bf16 parts each (2^-16 relative), and the
- * weights inside a block and the state as the block's queries read it are rounded to bf16 (2^-8).  Outputs
- * are rounded to bf16.  A token's output depends on no later token's numbers, NaN and infinities included.
+ * in fp32; longer ones in blocks of 64 tokens on bf16 matrix instructions with fp32 accumulation.  What
+ * enters the state there, values times decays, keeps its 24 bits as three bf16 parts; the weights inside a
+ * block, and the state as the block's queries read it, are rounded to bf16 (2^-8), which is what the bf16
+ * outputs are rounded to.  A token's output depends on no later token's numbers, NaN and infinities
+ * included; a state that an infinity has entered in a block holds NaN where it did.
  *
  * Call order on one stream, per wave: wavepp_lin_plan (host only) -> wavepp_lin_upload -> wavepp_lin_chunked_prefill
  * (once per layer, each with its own tensors and state pool).  A plan of single tokens that resume in place serves every

@@ -48,6 +48,17 @@ __device__ __forceinline__ bf16x8 acc_operand(const f32x4& a, const f32x4& b) {
   return r;
 }
 
+// Two fp32 values as three bf16 each, 8 bits of the value a part: word u of the parts' operands.  Cutting off instead of
+// rounding costs an instruction less a value and leaves the last part exact.
+__device__ __forceinline__ void split_pair(float x0, float x1, int u, u32x4& hi, u32x4& mid, u32x4& lo) {
+  auto upper = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); };
+  auto rest = [](float a) { return a - __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); };
+  const float y0 = rest(x0), y1 = rest(x1);
+  hi[u] = upper(x0, x1);
+  mid[u] = upper(y0, y1);
+  lo[u] = upper(rest(y0), rest(y1));
+}
+
 // The value of another lane of the same 16; where there is none, 1.
 template <int CTRL>
 __device__ __forceinline__ float row_or_one(float x) {
@@ -331,7 +342,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     const __bf16* vl = &b.v[(4 * g + (l16 >> 2)) * VS + 16 * wave + 4 * (l16 & 3)];
 #pragma unroll
     for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 16) * VS));
-    // S = lam_64 S + K^T (w V): the weighted values as two bf16 parts, which leave the state right to 2^-16
+    // S = lam_64 S + K^T (w V): the weighted values as three bf16 parts, 24 bits, so that the state is as exact as in fp32
     const float gamma = b.gamma;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
@@ -341,19 +352,22 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 4 * g]), w1 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 16 + 4 * g]);
-      bf16x8 hi, lo;
+      u32x4 hi, mid, lo;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float x = float(vf[t][e]) * (e < 4 ? w0[e & 3] : w1[e & 3]);
-        hi[e] = static_cast<__bf16>(x);
-        lo[e] = static_cast<__bf16>(x - float(hi[e]));
+      for (int u = 0; u < 4; ++u) {
+        const f32x4 w = u < 2 ? w0 : w1;
+        split_pair(float(vf[t][2 * u]) * w[2 * u & 3], float(vf[t][2 * u + 1]) * w[(2 * u + 1) & 3], u, hi, mid, lo);
       }
+      // part by part: no product waits for the sum of the one before it
+      bf16x8 kt[CT];
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        const bf16x8 kt = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 16) * KS + 16 * c));
-        S[c] = mfma(kt, hi, S[c]);
-        S[c] = mfma(kt, lo, S[c]);
-      }
+      for (int c = 0; c < CT; ++c) kt[c] = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 16) * KS + 16 * c));
+#pragma unroll
+      for (int c = 0; c < CT; ++c) S[c] = mfma(kt[c], __builtin_bit_cast(bf16x8, hi), S[c]);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) S[c] = mfma(kt[c], __builtin_bit_cast(bf16x8, mid), S[c]);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) S[c] = mfma(kt[c], __builtin_bit_cast(bf16x8, lo), S[c]);
     }
     pending = !AHEAD;
     if constexpr (!AHEAD) {
