@@ -745,188 +745,217 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   // chunks: the wave is bound by streaming the prefix K/V), half of those waves would idle: the
   // plan then uses 128-row items, run by the 4-wave form of the kernel, two workgroups per CU.
   // WAVEPP_GQA_WAVES=4 or 8 forces one form.
-  int64_t max_rows = 0;
-  for (int32_t r = 0; r < R; ++r) max_rows = std::max<int64_t>(max_rows, int64_t(batch->chunk_lens[r]) * (s.num_q_heads / s.num_kv_heads));
+  // Over 4-bit pages, requests of up to 32 rows a KV head -- a token or a few -- run with one wave's rows and the
+  // keys of a tile shared out over the four waves of a workgroup, in a launch of their own beside longer chunks.
   const char* gw = getenv("WAVEPP_GQA_WAVES");
   const int gw_n = gw ? atoi(gw) : 0;
+  auto rows_of = [&](int32_t r) { return int64_t(batch->chunk_lens[r]) * G; };
+  auto is_few = [&](int32_t r) { return q4 && gw_n == 0 && rows_of(r) <= kQ4FewRows; };
+  int64_t max_rows = 0;
+  bool any_few = false;
+  for (int32_t r = 0; r < R; ++r) {
+    if (is_few(r)) any_few = any_few || batch->chunk_lens[r] > 0;
+    else max_rows = std::max(max_rows, rows_of(r));
+  }
+  const bool any_many = max_rows > 0;
   const bool small_rows = gw_n == 4 || (gw_n != 8 && max_rows <= kGqaRowsPerItem / 2);
-  // Over 4-bit pages, up to 32 rows for every (request, KV head) -- a token or a few -- run with one wave's rows and
-  // the keys of a tile shared out over the four waves of a workgroup.
-  const bool few_rows = q4 && gw_n == 0 && max_rows <= kQ4FewRows;
-  const int gqa_rows = few_rows ? kQ4FewRows : small_rows ? kGqaRowsPerItem / 2 : kGqaRowsPerItem;
-  const int M = mla ? kMlaRowsPerItem : gqa_rows;
-  // keys per tile of the kernel that will run the plan (the 4-wave grouped form uses half tiles);
-  // split boundaries fall on whole tiles of it
-  const int KT = mla ? kMlaKvTile : few_rows ? kQ4FewTile : (small_rows ? kKvTile / 2 : kKvTile);
-  plan->rows_per_item = M;
-  plan->kv_tile = KT;
-
-  // --- work items --------------------------------------------------------------------------------
-  std::vector<WorkItem> base;
   std::vector<ReqMeta> reqs(R);
   int64_t cu = 0;
   for (int32_t r = 0; r < R; ++r) {
-    const int32_t p = batch->prefix_lens[r], c = batch->chunk_lens[r];
-    reqs[r] = ReqMeta{p, c, int32_t(cu), int32_t(int64_t(r) * stride)};
-    cu += c;
-    const int64_t rows_total = int64_t(c) * G;
-    for (int32_t g = 0; g < s.num_kv_heads; ++g)
-      for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
-        WorkItem w{};
-        w.req = r;
-        w.kv_head = g;
-        w.row0 = int32_t(r0);
-        w.rows = int32_t(std::min<int64_t>(M, rows_total - r0));
-        const int64_t last_tok = (r0 + w.rows - 1) / G;
-        w.kv_begin = 0;
-        w.kv_end = int32_t(p + last_tok + 1);
-        w.part = -1;
-        w.split = 0;
-        base.push_back(w);
-      }
+    reqs[r] = ReqMeta{batch->prefix_lens[r], batch->chunk_lens[r], int32_t(cu), int32_t(int64_t(r) * stride)};
+    cu += batch->chunk_lens[r];
   }
-  // key-range splits: forced by max_splits, or chosen so that a small wave still fills the chip,
-  // an item's automatic splits sharing its tiles evenly, 1,024 keys (grouped kernel) or 512
-  // (latent kernel) each or more; only an item's last split can be shorter.
-  // Split a wave with fewer base items than this until it has about that many.  512 items are two
-  // workgroups per CU of the 4-wave form, or two rounds of the one-per-CU forms; on the short-chunk
-  // waves (c = 16 .. 128) it gave the fastest or within 0.5 % of the fastest split count, against
-  // 1,024 items, which cost 2-11 % in the extra partials and merge work.
-  // Automatic splits share the wave's tiles out evenly rather than giving every (request, KV head,
-  // row tile) the same number of splits: such a wave runs as one round of workgroups and lasts as
-  // long as its longest item, so requests with longer prefixes take more splits.
-  const int64_t fill_target = 512;
-  const int64_t min_split_tiles = (mla ? 512 : few_rows ? 256 : 1024) / KT;
-  std::vector<int64_t> ntiles(base.size());
-  for (size_t i = 0; i < base.size(); ++i) ntiles[i] = ceil_div(base[i].kv_end, KT);
-  SplitPlan split{ntiles, int64_t(base.size())};
-  if (max_splits >= 1) {
-    for (size_t i = 0; i < base.size(); ++i) split.tps[i] = ceil_div(ntiles[i], std::min<int64_t>(max_splits, ntiles[i]));
-  } else if (few_rows) {
-    split = few_rows_split(ntiles, fill_target, min_split_tiles);
-  } else if (int64_t(base.size()) < fill_target) {
-    auto auto_splits = [&](int64_t n, int64_t T) {       // (32-bit divisions: this runs a dozen times an item)
-      return std::max<int64_t>(1, std::min(uint32_t(n + T - 1) / uint32_t(T), uint32_t(n) / uint32_t(min_split_tiles)));
-    };
-    const int64_t longest = base.empty() ? 1 : *std::max_element(ntiles.begin(), ntiles.end());
-    // even splits of at most `target` items: the smallest T (no shorter than the minimum) that keeps to it;
-    // the number of items does not grow with T, and with T = longest it is base.size() < fill_target
-    auto even = [&](int64_t target) {
-      auto total = [&](int64_t T) {
-        int64_t n = 0;
-        for (int64_t t : ntiles) n += auto_splits(t, T);
-        return n;
-      };
-      int64_t lo = std::max<int64_t>(1, min_split_tiles), hi = std::max(lo, longest);
-      if (total(lo) > target) {
-        while (hi - lo > 1) {
-          const int64_t mid = lo + (hi - lo) / 2;
-          if (total(mid) <= target) hi = mid; else lo = mid;
-        }
-        lo = hi;
-      }
-      SplitPlan sp;
-      sp.tps.reserve(ntiles.size());
-      for (int64_t t : ntiles) {
-        const uint32_t n = uint32_t(t), splits = uint32_t(auto_splits(t, lo)), tps = (n + splits - 1) / splits;
-        sp.tps.push_back(tps);
-        sp.pieces += (n + tps - 1) / tps;
-      }
-      return sp;
-    };
-    // The 8-wave grouped form also runs one workgroup per CU; a wave split to 512 items is two rounds of it.  Its
-    // 256 slots are filled once where the model gives that more than 5 %, its mean error: 1.03 to 1.28 times
-    // faster wherever it says so on the timed waves (one request of 8K-40K cached tokens, 64/8 heads, 304 rows
-    // per KV head: 67.5 us as 352 items, 54.6 as 256), while 256 items always would lose 15 % on average.
-    int64_t target = fill_target;
-    if (!mla && !small_rows && int64_t(base.size()) < kNumCu && longest >= 2 * min_split_tiles &&
-        grouped_cost(s, *batch, kNumCu, 1024) < 0.95 * grouped_cost(s, *batch, fill_target, 1024))
-      target = kNumCu;
-    split = even(target);
-    // The latent form runs one workgroup per CU: 256 slots, not 512, and its partials are four times as wide.
-    // For it the alternatives are even splits of at most 256 items, and pieces of about the mean load per
-    // slot: whole pieces fill most slots and the items' remainders pair up on the others.  The cheapest by
-    // split_cost is taken.  Measured on 12 requests of 4K-16K cached and 1-12 new tokens, 128 heads: 254 us with
-    // the 512-item split, 243 with 256 even items.  The overheads are a piece's prologue and epilogue in
-    // tiles, and the merge's share of a piece's partial rows at about 5 TB/s.
-    if (mla && longest >= 2 * min_split_tiles) {
-      const int slots = kNumCu;
-      const double overhead = 5.0, merge = 0.015;
-      double best = split_cost(ntiles, split, overhead, merge, INFINITY);
-      auto consider = [&](SplitPlan sp) {
-        if (sp.pieces > fill_target) return;
-        const double c = split_cost(ntiles, sp, overhead, merge, best);
-        if (c < best) {
-          best = c;
-          split = std::move(sp);
-        }
-      };
-      if (int64_t(base.size()) < slots) consider(even(slots));
-      const int64_t sum = std::accumulate(ntiles.begin(), ntiles.end(), int64_t(0));
-      int64_t last = 0;
-      for (double f : {1.0, 1.04, 1.08, 1.15, 1.25}) {
-        const int64_t T = std::max<int64_t>(min_split_tiles, int64_t(std::ceil(f * double(sum) / slots)));
-        if (T == last) continue;
-        last = T;
-        SplitPlan sp;
-        sp.tps.reserve(ntiles.size());
-        for (int64_t tiles : ntiles) {
-          const uint32_t n = uint32_t(tiles);
-          uint32_t t = std::min(uint32_t(T), n), whole = n / t, left = n - whole * t;
-          // a remainder below the minimum split length is shared out over the whole pieces, once: the new last piece
-          // can be short too (100 tiles: 11 pieces of 9 and one of 1).  Longer pieces until none is short: the
-          // same time over 60 waves that it changes, single ones 9 % slower to 3 % faster.
-          if (left && left < min_split_tiles) {
-            t = (n + whole - 1) / whole;
-            whole = n / t;
-            left = n - whole * t;
-          }
-          sp.tps.push_back(t);
-          sp.pieces += whole + (left != 0);
-        }
-        consider(std::move(sp));
-      }
-    }
+  // the requests that are not few, for the model of grouped waves
+  std::vector<int32_t> many_lens;
+  wavepp_batch many = *batch;
+  if (any_few && any_many) {
+    many_lens.assign(batch->chunk_lens, batch->chunk_lens + R);
+    for (int32_t r = 0; r < R; ++r)
+      if (is_few(r)) many_lens[r] = 0;
+    many.chunk_lens = many_lens.data();
   }
-  std::vector<WorkItem> items;
   int64_t part_rows = 0;
   int max_used = 1;
-  for (size_t bi = 0; bi < base.size(); ++bi) {
-    const WorkItem& w = base[bi];
-    const int64_t tps = split.tps[bi], S = ceil_div(ntiles[bi], tps);
-    if (S == 1) {
-      items.push_back(w);
-      continue;
+
+  // --- work items of the requests that are few, or of the others: WAVEPP_OK, or what stands against it -------------
+  auto plan_items = [&](const bool few_rows) {
+    const int gqa_rows = few_rows ? kQ4FewRows : small_rows ? kGqaRowsPerItem / 2 : kGqaRowsPerItem;
+    const int M = mla ? kMlaRowsPerItem : gqa_rows;
+    // keys per tile of the kernel that will run the plan (the 4-wave grouped form uses half tiles);
+    // split boundaries fall on whole tiles of it
+    const int KT = mla ? kMlaKvTile : few_rows ? kQ4FewTile : (small_rows ? kKvTile / 2 : kKvTile);
+    if (!few_rows || !any_many) {
+      plan->rows_per_item = M;
+      plan->kv_tile = KT;
     }
-    max_used = std::max<int>(max_used, int(S));
-    MergeItem m{};
-    m.req = w.req;
-    m.kv_head = w.kv_head;
-    m.row0 = w.row0;
-    m.rows = w.rows;
-    m.nsplit = int32_t(S);
-    m.part = int32_t(part_rows);
-    plan->merges.push_back(m);
-    for (int64_t si = 0; si < S; ++si) {
-      WorkItem x = w;
-      x.kv_begin = int32_t(si * tps * KT);
-      x.kv_end = int32_t(std::min<int64_t>(w.kv_end, (si + 1) * tps * KT));
-      x.part = int32_t(part_rows + si * w.rows);
-      x.split = int32_t(si);
-      items.push_back(x);
+    std::vector<WorkItem> base;
+    for (int32_t r = 0; r < R; ++r) {
+      if (is_few(r) != few_rows) continue;
+      const int32_t p = batch->prefix_lens[r];
+      const int64_t rows_total = rows_of(r);
+      for (int32_t g = 0; g < s.num_kv_heads; ++g)
+        for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
+          WorkItem w{};
+          w.req = r;
+          w.kv_head = g;
+          w.row0 = int32_t(r0);
+          w.rows = int32_t(std::min<int64_t>(M, rows_total - r0));
+          const int64_t last_tok = (r0 + w.rows - 1) / G;
+          w.kv_begin = 0;
+          w.kv_end = int32_t(p + last_tok + 1);
+          w.part = -1;
+          w.split = 0;
+          base.push_back(w);
+        }
     }
-    part_rows += S * w.rows;
-    if (part_rows > INT32_MAX / 2) return set_error(WAVEPP_EINVAL, "split partials too large");
-  }
-  plan->num_real_items = int32_t(items.size());
+    // key-range splits: forced by max_splits, or chosen so that a small wave still fills the chip,
+    // an item's automatic splits sharing its tiles evenly, 1,024 keys (grouped kernel) or 512
+    // (latent kernel) each or more; only an item's last split can be shorter.
+    // Split a wave with fewer base items than this until it has about that many.  512 items are two
+    // workgroups per CU of the 4-wave form, or two rounds of the one-per-CU forms; on the short-chunk
+    // waves (c = 16 .. 128) it gave the fastest or within 0.5 % of the fastest split count, against
+    // 1,024 items, which cost 2-11 % in the extra partials and merge work.
+    // Automatic splits share the wave's tiles out evenly rather than giving every (request, KV head,
+    // row tile) the same number of splits: such a wave runs as one round of workgroups and lasts as
+    // long as its longest item, so requests with longer prefixes take more splits.
+    const int64_t fill_target = 512;
+    const int64_t min_split_tiles = (mla ? 512 : few_rows ? 256 : 1024) / KT;
+    std::vector<int64_t> ntiles(base.size());
+    for (size_t i = 0; i < base.size(); ++i) ntiles[i] = ceil_div(base[i].kv_end, KT);
+    SplitPlan split{ntiles, int64_t(base.size())};
+    if (max_splits >= 1) {
+      for (size_t i = 0; i < base.size(); ++i) split.tps[i] = ceil_div(ntiles[i], std::min<int64_t>(max_splits, ntiles[i]));
+    } else if (few_rows) {
+      split = few_rows_split(ntiles, fill_target, min_split_tiles);
+    } else if (int64_t(base.size()) < fill_target) {
+      auto auto_splits = [&](int64_t n, int64_t T) {       // (32-bit divisions: this runs a dozen times an item)
+        return std::max<int64_t>(1, std::min(uint32_t(n + T - 1) / uint32_t(T), uint32_t(n) / uint32_t(min_split_tiles)));
+      };
+      const int64_t longest = base.empty() ? 1 : *std::max_element(ntiles.begin(), ntiles.end());
+      // even splits of at most `target` items: the smallest T (no shorter than the minimum) that keeps to it;
+      // the number of items does not grow with T, and with T = longest it is base.size() < fill_target
+      auto even = [&](int64_t target) {
+        auto total = [&](int64_t T) {
+          int64_t n = 0;
+          for (int64_t t : ntiles) n += auto_splits(t, T);
+          return n;
+        };
+        int64_t lo = std::max<int64_t>(1, min_split_tiles), hi = std::max(lo, longest);
+        if (total(lo) > target) {
+          while (hi - lo > 1) {
+            const int64_t mid = lo + (hi - lo) / 2;
+            if (total(mid) <= target) hi = mid; else lo = mid;
+          }
+          lo = hi;
+        }
+        SplitPlan sp;
+        sp.tps.reserve(ntiles.size());
+        for (int64_t t : ntiles) {
+          const uint32_t n = uint32_t(t), splits = uint32_t(auto_splits(t, lo)), tps = (n + splits - 1) / splits;
+          sp.tps.push_back(tps);
+          sp.pieces += (n + tps - 1) / tps;
+        }
+        return sp;
+      };
+      // The 8-wave grouped form also runs one workgroup per CU; a wave split to 512 items is two rounds of it.  Its
+      // 256 slots are filled once where the model gives that more than 5 %, its mean error: 1.03 to 1.28 times
+      // faster wherever it says so on the timed waves (one request of 8K-40K cached tokens, 64/8 heads, 304 rows
+      // per KV head: 67.5 us as 352 items, 54.6 as 256), while 256 items always would lose 15 % on average.
+      int64_t target = fill_target;
+      if (!mla && !small_rows && int64_t(base.size()) < kNumCu && longest >= 2 * min_split_tiles &&
+          grouped_cost(s, many, kNumCu, 1024) < 0.95 * grouped_cost(s, many, fill_target, 1024))
+        target = kNumCu;
+      split = even(target);
+      // The latent form runs one workgroup per CU: 256 slots, not 512, and its partials are four times as wide.
+      // For it the alternatives are even splits of at most 256 items, and pieces of about the mean load per
+      // slot: whole pieces fill most slots and the items' remainders pair up on the others.  The cheapest by
+      // split_cost is taken.  Measured on 12 requests of 4K-16K cached and 1-12 new tokens, 128 heads: 254 us with
+      // the 512-item split, 243 with 256 even items.  The overheads are a piece's prologue and epilogue in
+      // tiles, and the merge's share of a piece's partial rows at about 5 TB/s.
+      if (mla && longest >= 2 * min_split_tiles) {
+        const int slots = kNumCu;
+        const double overhead = 5.0, merge = 0.015;
+        double best = split_cost(ntiles, split, overhead, merge, INFINITY);
+        auto consider = [&](SplitPlan sp) {
+          if (sp.pieces > fill_target) return;
+          const double c = split_cost(ntiles, sp, overhead, merge, best);
+          if (c < best) {
+            best = c;
+            split = std::move(sp);
+          }
+        };
+        if (int64_t(base.size()) < slots) consider(even(slots));
+        const int64_t sum = std::accumulate(ntiles.begin(), ntiles.end(), int64_t(0));
+        int64_t last = 0;
+        for (double f : {1.0, 1.04, 1.08, 1.15, 1.25}) {
+          const int64_t T = std::max<int64_t>(min_split_tiles, int64_t(std::ceil(f * double(sum) / slots)));
+          if (T == last) continue;
+          last = T;
+          SplitPlan sp;
+          sp.tps.reserve(ntiles.size());
+          for (int64_t tiles : ntiles) {
+            const uint32_t n = uint32_t(tiles);
+            uint32_t t = std::min(uint32_t(T), n), whole = n / t, left = n - whole * t;
+            // a remainder below the minimum split length is shared out over the whole pieces, once: the new last piece
+            // can be short too (100 tiles: 11 pieces of 9 and one of 1).  Longer pieces until none is short: the
+            // same time over 60 waves that it changes, single ones 9 % slower to 3 % faster.
+            if (left && left < min_split_tiles) {
+              t = (n + whole - 1) / whole;
+              whole = n / t;
+              left = n - whole * t;
+            }
+            sp.tps.push_back(t);
+            sp.pieces += whole + (left != 0);
+          }
+          consider(std::move(sp));
+        }
+      }
+    }
+    std::vector<WorkItem> items;
+    for (size_t bi = 0; bi < base.size(); ++bi) {
+      const WorkItem& w = base[bi];
+      const int64_t tps = split.tps[bi], S = ceil_div(ntiles[bi], tps);
+      if (S == 1) {
+        items.push_back(w);
+        continue;
+      }
+      max_used = std::max<int>(max_used, int(S));
+      MergeItem m{};
+      m.req = w.req;
+      m.kv_head = w.kv_head;
+      m.row0 = w.row0;
+      m.rows = w.rows;
+      m.nsplit = int32_t(S);
+      m.part = int32_t(part_rows);
+      plan->merges.push_back(m);
+      for (int64_t si = 0; si < S; ++si) {
+        WorkItem x = w;
+        x.kv_begin = int32_t(si * tps * KT);
+        x.kv_end = int32_t(std::min<int64_t>(w.kv_end, (si + 1) * tps * KT));
+        x.part = int32_t(part_rows + si * w.rows);
+        x.split = int32_t(si);
+        items.push_back(x);
+      }
+      part_rows += S * w.rows;
+      if (part_rows > INT32_MAX / 2) return set_error(WAVEPP_EINVAL, "split partials too large");
+    }
+    plan->num_real_items += int32_t(items.size());
+    // workgroups per CU: the 4-wave grouped form runs two, or three at head dim 64; the others one
+    const int per_cu = (small_rows || few_rows) && !mla ? (s.head_dim_qk == 64 ? 3 : 2) : 1;
+    items = order_items(std::move(items), G, env_flag("WAVEPP_XCD_ORDER", true),
+                        env_flag("WAVEPP_STREAM_MAJOR", true), per_cu * kNumCu, KT, mla ? 5.0 : 1.0,
+                        mla || small_rows || few_rows ? 1.0 : kModel128.idle);
+    if (few_rows) plan->num_few = int32_t(items.size());
+    plan->items.insert(plan->items.end(), items.begin(), items.end());
+    return int(WAVEPP_OK);
+  };
+  int st = any_many || !any_few ? plan_items(false) : int(WAVEPP_OK);
+  if (!st && any_few) st = plan_items(true);
+  if (st) return st;
   plan->max_splits_used = max_used;
   plan->partial_rows = part_rows;
   for (const MergeItem& m : plan->merges) plan->merge_rows = std::max(plan->merge_rows, m.rows);
   plan->num_merge_wide = merge_wide_items(plan->merges, plan->merge_rows, s.head_dim_v);
-  // workgroups per CU: the 4-wave grouped form runs two, or three at head dim 64; the others one
-  const int per_cu = small_rows && !mla ? (s.head_dim_qk == 64 ? 3 : 2) : 1;
-  plan->items = order_items(std::move(items), G, env_flag("WAVEPP_XCD_ORDER", true),
-                            env_flag("WAVEPP_STREAM_MAJOR", true), per_cu * kNumCu, KT, mla ? 5.0 : 1.0, mla || small_rows ? 1.0 : kModel128.idle);
   if (plan->items.size() > size_t(INT32_MAX / 2)) return set_error(WAVEPP_EINVAL, "too many work items");
 
   // --- metadata blob -------------------------------------------------------------------------------

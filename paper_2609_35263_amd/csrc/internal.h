@@ -202,8 +202,8 @@ hipError_t launch_q4_append(const DevPlan& p, const void* k_new, const void* v_n
                             hipStream_t stream);
 hipError_t launch_q4_read(const DevPlan& p, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                           hipStream_t stream);
-hipError_t launch_q4_attention(const DevPlan& p, const void* q, const void* k_pool, const void* v_pool, void* out,
-                               float* lse, hipStream_t stream);
+hipError_t launch_q4_attention(const DevPlan& p, int32_t num_few, const void* q, const void* k_pool, const void* v_pool,
+                               void* out, float* lse, hipStream_t stream);   // num_few: see wavepp_plan
 hipError_t launch_merge(const DevPlan& p, void* out, float* lse, hipStream_t stream);
 // Copy `bytes` (a multiple of 16, both pointers 16-byte aligned) from device-visible pinned host
 // memory to device memory with a kernel on `stream`.

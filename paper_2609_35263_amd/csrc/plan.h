@@ -18,6 +18,7 @@ struct wavepp_plan {
   int32_t kv_tile = 0;
   int32_t max_splits_used = 1;
   int32_t num_real_items = 0;
+  int32_t num_few = 0;                // the last items, which run with few rows over 4-bit pages
   std::vector<wavepp::WorkItem> items;
   std::vector<wavepp::MergeItem> merges;      // those that merge_wide_kernel takes first
   int32_t num_merge_wide = 0, merge_rows = 0;

@@ -701,23 +701,25 @@ hipError_t launch_q4_read(const DevPlan& p, const void* k_pool, const void* v_po
   return hipGetLastError();
 }
 
-hipError_t launch_q4_attention(const DevPlan& p, const void* q, const void* k_pool, const void* v_pool, void* out,
-                               float* lse, hipStream_t stream) {
+hipError_t launch_q4_attention(const DevPlan& p, int32_t num_few, const void* q, const void* k_pool, const void* v_pool,
+                               void* out, float* lse, hipStream_t stream) {
   if (p.num_items == 0) return hipSuccess;
   auto qq = static_cast<const __bf16*>(q);
   auto kp = static_cast<const uint8_t*>(k_pool);
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto oo = static_cast<__bf16*>(out);
-  const dim3 grid(p.num_items);
+  const int32_t num_many = p.num_items - num_few;
+  const bool w8 = p.rows_per_item == kGqaRowsPerItem;
+  if (num_many && !w8 && p.rows_per_item != kGqaRowsPerItem / 2) return hipErrorInvalidValue;
+  DevPlan few = p;
+  few.items += num_many;
 #define WAVEPP_Q4(D_, P_)                                                                                             \
-  if (p.rows_per_item == kGqaRowsPerItem)                                                                             \
-    hipLaunchKernelGGL((attn_q4_kernel<D_, P_, 8>), grid, dim3(512), 0, stream, p, qq, kp, vp, oo, lse);               \
-  else if (p.rows_per_item == kGqaRowsPerItem / 2)                                                                    \
-    hipLaunchKernelGGL((attn_q4_kernel<D_, P_, 4>), grid, dim3(256), 0, stream, p, qq, kp, vp, oo, lse);               \
-  else if (p.rows_per_item == kQ4FewRows)                                                                             \
-    hipLaunchKernelGGL((attn_q4_few_kernel<D_, P_>), grid, dim3(256), 0, stream, p, qq, kp, vp, oo, lse);              \
-  else                                                                                                                \
-    return hipErrorInvalidValue;
+  if (num_many && w8)                                                                                                 \
+    hipLaunchKernelGGL((attn_q4_kernel<D_, P_, 8>), dim3(num_many), dim3(512), 0, stream, p, qq, kp, vp, oo, lse);     \
+  else if (num_many)                                                                                                  \
+    hipLaunchKernelGGL((attn_q4_kernel<D_, P_, 4>), dim3(num_many), dim3(256), 0, stream, p, qq, kp, vp, oo, lse);     \
+  if (num_few)                                                                                                        \
+    hipLaunchKernelGGL((attn_q4_few_kernel<D_, P_>), dim3(num_few), dim3(256), 0, stream, few, qq, kp, vp, oo, lse);
   if (p.head_dim_qk == 128 && p.page_size == 64) {
     WAVEPP_Q4(128, 64)
   } else if (p.head_dim_qk == 128 && p.page_size == 16) {

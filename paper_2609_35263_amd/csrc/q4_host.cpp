@@ -78,7 +78,7 @@ int wavepp_q4_chunked_prefill(const wavepp_plan* plan, const void* q, const void
   if (st) return st;
   if (reinterpret_cast<uintptr_t>(lse) & 3) return set_error(WAVEPP_EINVAL, "lse must be 4-byte aligned");
   const DevPlan d = make_dev(plan, workspace);
-  hipError_t e = launch_q4_attention(d, q, k_pool, v_pool, out, lse, stream);
+  hipError_t e = launch_q4_attention(d, plan->num_few, q, k_pool, v_pool, out, lse, stream);
   if (e != hipSuccess) return set_hip_error(e, "q4 attention launch");
   if (!plan->merges.empty()) {
     e = launch_merge(d, out, lse, stream);

@@ -13,7 +13,7 @@ hipError_t launch_lin(const LinDevPlan&, const void*, const void*, const void*, 
 }
 hipError_t launch_q4_append(const DevPlan&, const void*, const void*, void*, void*, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_q4_read(const DevPlan&, const void*, const void*, void*, void*, hipStream_t) { return hipErrorNotSupported; }
-hipError_t launch_q4_attention(const DevPlan&, const void*, const void*, const void*, void*, float*, hipStream_t) {
+hipError_t launch_q4_attention(const DevPlan&, int32_t, const void*, const void*, const void*, void*, float*, hipStream_t) {
   return hipErrorNotSupported;
 }
 }  // namespace wavepp

@@ -154,6 +154,8 @@ WAVES = {
     "wide_group": (16, 1, 128, 64, [130], [7]),
     "eight_waves": (8, 2, 128, 64, [70, 0, 0], [150, 40, 65]),
     "eight_waves_small": (8, 2, 64, 16, [33, 5], [130, 70]),
+    "chunks_beside_tokens": (8, 2, 128, 64, [70, 700, 0, 300, 2000, 0], [150, 1, 40, 8, 0, 1]),
+    "short_chunks_beside_tokens": (24, 4, 64, 16, [900, 50, 17], [1, 17, 5]),
 }
 
 

@@ -46,6 +46,20 @@ def test_rows_of_an_item_follow_the_longest_chunk(chunk, heads, rows):
     assert p.info()["rows_per_item"] == rows
 
 
+def test_tokens_beside_chunks_have_items_of_their_own():
+    """Few-row requests come last, in tiles and splits as if alone."""
+    kw = dict(num_q_heads=16, num_kv_heads=2, head_dim_qk=128, head_dim_v=128, page_size=64, num_pages=400, softmax_scale=1.0,
+              block_table=np.arange(400).reshape(4, 100))
+    p = wp.q4_plan(prefix_lens=[5000, 100, 3000, 64], chunk_lens=[1, 300, 2, 0], **kw)
+    items = p.items()
+    few = np.isin(items[:, 0], [0, 2]) & (items[:, 3] > 0)
+    assert p.info()["rows_per_item"] == 256 and few.any() and items[few][:, 3].max() == 16
+    first = np.flatnonzero(few)[0]
+    assert not ((items[first:, 3] > 0) & ~few[first:]).any()
+    alone = wp.q4_plan(prefix_lens=[5000, 100, 3000, 64], chunk_lens=[1, 0, 2, 0], **kw).items()
+    assert sorted(map(tuple, alone[alone[:, 3] > 0][:, [0, 1, 2, 3, 4, 5]])) == sorted(map(tuple, items[few][:, [0, 1, 2, 3, 4, 5]]))
+
+
 @pytest.mark.parametrize("seed", range(8))
 def test_items_cover_every_visible_key_of_every_row_once(seed):
     rng = np.random.default_rng(seed)
