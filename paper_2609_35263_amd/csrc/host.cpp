@@ -8,6 +8,7 @@
 #include "wavepp_attn.h"
 #include "internal.h"
 #include "plan.h"
+#include "q4.h"
 
 #include <hip/hip_runtime.h>
 

@@ -15,9 +15,6 @@ constexpr int kNumXcd = 8;                 // L2 domains a launch is spread over
 constexpr int kNumEngines = 32;            // shader engines, which workgroups go to in turn
 constexpr int kMlaRowsPerItem = 128;       // latent kernel: query rows per work item
 constexpr int kMlaKvTile = 64;             // latent kernel: keys per tile
-constexpr int kQ4FewRows = 32;             // 4-bit pages, few rows: query rows per work item (every wave has them all)
-constexpr int kQ4FewTile = 128;            // 4-bit pages, few rows: keys per step of a workgroup, 32 a wave
-constexpr int kQ4Block = 32;               // values along the head dim that share a scale
 constexpr int kMergeNarrow = 16;           // merge: splits whose partials one thread loads at once
 
 // Header at the start of the uploaded metadata.
@@ -108,62 +105,9 @@ struct alignas(16) KdaItem {
   int32_t pad[3];
 };
 
-// ---------------------------------------------------------------------------------------------
-// Linear attention with a decay for each head
-// ---------------------------------------------------------------------------------------------
-constexpr uint32_t kLinMagic = 0x4C494E31u;  // "LIN1"
-constexpr int kLinBlock = 64;                // tokens per block of the chunkwise form
-// Chunks up to this length run token by token: 64 requests of 64 heads of 128 x 128 take 128 us so and 154 in blocks at
-// eight tokens, 159 and 156 at twelve, 197 and 158 at sixteen; 4 of 32 of 128 x 64: 7.1 and 9.0, 8.9 and 9.2, 11.1 and 9.1.
-constexpr int kLinStepTokens = 10;
-
-struct alignas(16) LinHeader {
-  uint32_t magic;
-  uint32_t serial;
-  int32_t num_steps;
-  int32_t num_segments;
-};
-
-// A run of tokens of one request: a whole short chunk (token by token), or a segment of a longer one (whole blocks but
-// for the request's last).  States are snapshot slots, or partial states of the workspace between segments.
-struct alignas(16) LinItem {
-  int32_t cu;         // first packed token
-  int32_t len;        // > 0
-  int32_t state_in;   // snapshot slot to start from, -1 = zero state (with part_in < 0)
-  int32_t state_out;  // snapshot slot written at the end, -1 = none
-  int32_t part_in;    // >= 0: start from this partial state instead
-  int32_t part_out;   // >= 0: where this segment's own state goes
-  int32_t pad[2];
-};
-
-// The partial states of one request's segments, in order.
-struct alignas(16) LinScan {
-  int32_t state_in;   // the first segment's start
-  int32_t first_part;
-  int32_t count;
-  int32_t start_part; // >= 0: the start is copied here, for the first segment of a request whose last writes the same slot
-};
-
-struct LinDevPlan {
-  const LinHeader* hdr;
-  const LinItem* steps;
-  const LinItem* segments;   // those with part_out >= 0 first
-  const LinScan* scans;
-  float* parts;              // [partial states][num_heads][head_dim_k][head_dim_v]
-  float* part_decay;         // [partial states][num_heads]
-  uint32_t serial;
-  int32_t num_steps, num_segments, num_ahead, num_scans;
-  int32_t num_heads, num_qk_heads, head_dim_k, head_dim_v, alpha_per_token;
-  float scale;
-};
-
-hipError_t launch_lin(const LinDevPlan& p, const void* q, const void* k, const void* v, const float* alpha,
-                      float* state_pool, void* out, hipStream_t stream);
-
 // The metadata upload copies 16-byte words, so every record of a blob is a multiple of 16 bytes.
 static_assert(sizeof(MetaHeader) % 16 == 0 && sizeof(ReqMeta) % 16 == 0 && sizeof(WorkItem) % 16 == 0 &&
-                  sizeof(MergeItem) % 16 == 0 && sizeof(KdaHeader) % 16 == 0 && sizeof(KdaItem) % 16 == 0 &&
-                  sizeof(LinHeader) % 16 == 0 && sizeof(LinItem) % 16 == 0 && sizeof(LinScan) % 16 == 0,
+                  sizeof(MergeItem) % 16 == 0 && sizeof(KdaHeader) % 16 == 0 && sizeof(KdaItem) % 16 == 0,
               "metadata records are whole 16-byte words");
 
 struct KdaDevPlan {
@@ -197,13 +141,6 @@ hipError_t launch_append(const DevPlan& p, const void* k_new, const void* v_new,
                          hipStream_t stream);
 hipError_t launch_attention(const DevPlan& p, const void* q, const void* k_pool, const void* v_pool, void* out,
                             float* lse, hipStream_t stream);
-// The same over 4-bit pages, and the way back from them to bf16 rows.
-hipError_t launch_q4_append(const DevPlan& p, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
-                            hipStream_t stream);
-hipError_t launch_q4_read(const DevPlan& p, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
-                          hipStream_t stream);
-hipError_t launch_q4_attention(const DevPlan& p, int32_t num_few, const void* q, const void* k_pool, const void* v_pool,
-                               void* out, float* lse, hipStream_t stream);   // num_few: see wavepp_plan
 hipError_t launch_merge(const DevPlan& p, void* out, float* lse, hipStream_t stream);
 // Copy `bytes` (a multiple of 16, both pointers 16-byte aligned) from device-visible pinned host
 // memory to device memory with a kernel on `stream`.

@@ -13,10 +13,19 @@
 // order, so the state feeds O^T = S0^T Q^T from registers, Q rows being read from LDS in that order; V and K^T
 // are read by transposing LDS reads.  The ten 16 x 16 tiles of (Q K^T) * D on and under the diagonal are shared out over
 // the waves and go through LDS.  The next block's rows are loaded while a block is worked on.
+//
+// What bounds it.  A block of 128 + 128 columns is 64 KiB of memory traffic, 3.4 us of a CU's share of a copy's rate; a
+// block's work is a chain of LDS reads, products and a barrier of about 3.1 us.  4 x 4,096 tokens, 64 heads of 128 x 128, one
+// workgroup on each of 256 CUs: 271 us, 4.1 TB/s where a large copy reaches 4.75 (232 us); 244 us without the products, 200
+// without the memory.  Measured on the way there (same wave): four waves of 32 columns that keep the logits in registers
+// 1,092 us (spills); eight of 16 with P in LDS 355; one barrier a block in place of three 325; Q and P in operand order, K's
+// pieces swapped 289 (the first bank conflicts took half the LDS's cycles); loads without branches 278; P before the rest
+// 269.  Not kept: two blocks of rows on their way (297: the registers spill), two workgroups of 64 columns a CU (352
+// against 289 then), the move of the next block to LDS first in a block (298), stores past the caches (361).
 #include <hip/hip_runtime.h>
 
 #include "device.h"
-#include "internal.h"
+#include "lin.h"
 
 #include <algorithm>
 
@@ -101,7 +110,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rows(const T* base, uint
 
 // An item by scalar loads (the kernels never write the metadata), so that the compiler knows it is uniform.
 __device__ __forceinline__ LinItem item_at(const LinItem* at) {
-  struct Halves { u32x4 a, b; } x = {const_load(reinterpret_cast<const u32x4*>(at)), const_load(reinterpret_cast<const u32x4*>(at) + 1)};
+  const u32x4* words = reinterpret_cast<const u32x4*>(at);
+  struct Halves { u32x4 a, b; } x = {const_load(words), const_load(words + 1)};
   return __builtin_bit_cast(LinItem, x);
 }
 
@@ -114,7 +124,9 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 }
 
 // ---------------------------------------------------------------------------------------------
-// Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.
+// Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.  Two blocks lie in LDS where d_v is
+// 128 (one workgroup of eight waves a CU), one where it is 64 (two of four waves: 207 -> 170 us on three ragged prompts, 32
+// heads of 128 x 64).
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, bool AHEAD>
 __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
@@ -179,9 +191,15 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
   // compiler knows how many are in flight and waits for the oldest block alone.
   uint32_t qk_off[KL], v_off[VL];
 #pragma unroll
-  for (int i = 0; i < KL; ++i) qk_off[i] = uint32_t((tid + NT * i) / (DK / 8) * Hqk * DK + (tid + NT * i) % (DK / 8) * 8) * 2;
+  for (int i = 0; i < KL; ++i) {
+    const int c = tid + NT * i;
+    qk_off[i] = uint32_t(c / (DK / 8) * Hqk * DK + c % (DK / 8) * 8) * 2;
+  }
 #pragma unroll
-  for (int i = 0; i < VL; ++i) v_off[i] = uint32_t((tid + NT * i) / (DV / 8) * H * DV + (tid + NT * i) % (DV / 8) * 8) * 2;
+  for (int i = 0; i < VL; ++i) {
+    const int c = tid + NT * i;
+    v_off[i] = uint32_t(c / (DV / 8) * H * DV + c % (DV / 8) * 8) * 2;
+  }
   const uint32_t a_row = p.alpha_per_token ? uint32_t(H) * 4 : 0;
   auto load = [&](Rows& x, int t0) {
     const int rows = __builtin_amdgcn_readfirstlane(max(0, min(kC, it.len - t0)));
@@ -256,7 +274,8 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
         row_table(a, l16, 0.0f, d);
 #pragma unroll
         for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) = f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]} * p.scale;
+          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) =
+              f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]} * p.scale;
       }
     }
   };
@@ -268,7 +287,8 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
   bf16x8 vf[2];
   const uint32_t o_off = uint32_t(l16 * H * DV + 16 * wave + 4 * g) * 2;
   auto put = [&](int t0) {
-    const auto ob = block_rows(out + (int64_t(it.cu + t0) * H + head) * DV, __builtin_amdgcn_readfirstlane(min(kC, it.len - t0)) * uint32_t(H * DV * 2));
+    const int rows = __builtin_amdgcn_readfirstlane(min(kC, it.len - t0));
+    const auto ob = block_rows(out + (int64_t(it.cu + t0) * H + head) * DV, rows * uint32_t(H * DV * 2));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       bf16x4 x;
@@ -301,8 +321,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
         const int ti = tile < 1 ? 0 : tile < 3 ? 1 : tile < 6 ? 2 : 3, tj = tile - ti * (ti + 1) / 2;
         f32x4 x = f32x4{};                                 // K Q^T: keys 4 g .. + 3 of query l16
 #pragma unroll
-        for (int s = 0; s < CT / 2; ++s)
-        {
+        for (int s = 0; s < CT / 2; ++s) {
           const __bf16* kr = &b.k[(16 * tj + l16) * KS + 32 * s + ((4 * g) ^ (l16 & 8))];
           x = mfma(cat(*reinterpret_cast<const bf16x4*>(kr), *reinterpret_cast<const bf16x4*>(kr + 16)),
                    operand(b.q, (16 * ti + l16) * QS + 32 * s + 8 * g), x);
@@ -351,7 +370,8 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     const __bf16* kl = &b.k[(4 * g + (l16 >> 2)) * KS + ((4 * (l16 & 3)) ^ (4 * g & 8))];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 4 * g]), w1 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 16 + 4 * g]);
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 4 * g]);
+      const f32x4 w1 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 16 + 4 * g]);
       u32x4 hi, mid, lo;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -361,7 +381,8 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
       // part by part: no product waits for the sum of the one before it
       bf16x8 kt[CT];
 #pragma unroll
-      for (int c = 0; c < CT; ++c) kt[c] = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 16) * KS + 16 * c));
+      for (int c = 0; c < CT; ++c)
+        kt[c] = cat(lds_read_tr(kl + 32 * t * KS + 16 * c), lds_read_tr(kl + (32 * t + 16) * KS + 16 * c));
 #pragma unroll
       for (int c = 0; c < CT; ++c) S[c] = mfma(kt[c], __builtin_bit_cast(bf16x8, hi), S[c]);
 #pragma unroll
@@ -436,7 +457,9 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinDevPlan p, const float
 
 // ---------------------------------------------------------------------------------------------
 // Token by token, in fp32.  A workgroup has 32 columns of one (request, head)'s state in registers: thread (row group,
-// column quad).  The outputs' sums over the rows are joined in LDS.
+// column quad).  The outputs' sums over the rows are joined in LDS.  A token each of 128 requests, 64 heads of 128 x 128, is
+// 1.08 GB of states read and written: 215 us, 5.0 TB/s, above a large copy's rate.  Few chains make up for their number by
+// the four workgroups that share a state (4 requests, 32 heads of 128 x 64: 4 us).
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV>
 __global__ __launch_bounds__(256) void lin_step_kernel(LinDevPlan p, const __bf16* __restrict__ q,

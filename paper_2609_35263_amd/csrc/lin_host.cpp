@@ -3,7 +3,7 @@
 // Resume semantics and the rules for slots are those of the KDA layers (kda_host.cpp): a wave's workgroups run
 // concurrently, so a slot that one request writes may be neither read nor written by another.
 #include "wavepp_lin.h"
-#include "internal.h"
+#include "lin.h"
 
 #include <hip/hip_runtime.h>
 

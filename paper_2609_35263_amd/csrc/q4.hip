@@ -8,7 +8,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device.h"
-#include "internal.h"
+#include "q4.h"
 
 #include <algorithm>
 
@@ -169,6 +169,10 @@ __global__ __launch_bounds__(256) void q4_read_kernel(DevPlan p, const uint8_t* 
 // and O^T += V^T P^T on 32x32x16 matrix instructions, K from LDS rows, V by transposing LDS reads, the probabilities
 // straight from the accumulators.  A tile's codes are loaded (a quarter of the bytes, 8 registers a thread) before
 // the MFMAs of the tile before it and turned into bf16 rows in the other LDS buffer after them: once for all NW waves.
+// It is bound by the matrix instructions and the softmax's VALU work beside them, as over bf16 pages: 1,024 tokens behind 65,536
+// (64/8 heads of 128) 1,834 us, 1.22 PFLOP/s where a large library product reaches 1.34 (1,885 us with V's pieces in order,
+// see v_place).  8 x 16 tokens behind 16-32 K: 136 us, four waves, twice the dequantisation for a row; the memory would
+// take 48.
 // ---------------------------------------------------------------------------------------------
 template <int D, int PAGE, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPlan p, const __bf16* __restrict__ q,
@@ -237,11 +241,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
     const uint32_t off = uint32_t(j % PAGE) * Page::ROW + part * (W * 4);
     const uint32_t soff = Page::CODES + uint32_t(j % PAGE) * Page::NB + part * Page::NB / 4;
     if constexpr (W == 4) {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(kpool_h + at + off), b = *reinterpret_cast<const u32x4*>(vpool_h + at + off);
+      const u32x4 a = *reinterpret_cast<const u32x4*>(kpool_h + at + off);
+      const u32x4 b = *reinterpret_cast<const u32x4*>(vpool_h + at + off);
 #pragma unroll
       for (int i = 0; i < W; ++i) kreg[i] = a[i], vreg[i] = b[i];
     } else {
-      const u32x2 a = *reinterpret_cast<const u32x2*>(kpool_h + at + off), b = *reinterpret_cast<const u32x2*>(vpool_h + at + off);
+      const u32x2 a = *reinterpret_cast<const u32x2*>(kpool_h + at + off);
+      const u32x2 b = *reinterpret_cast<const u32x2*>(vpool_h + at + off);
 #pragma unroll
       for (int i = 0; i < W; ++i) kreg[i] = a[i], vreg[i] = b[i];
     }
@@ -265,14 +271,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
   int v_lane[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
-    v_lane[db] = (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 4 * (lane & 1);
+    v_lane[db] = (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) +
+                 4 * (lane & 1);
 
   const int t_begin = it.kv_begin / KT;
   const int t_end = (it.kv_end + KT - 1) / KT;
-  {
-    load_tile(t_begin, page_of(t_begin));
-    store_tile(0);
-  }
+  load_tile(t_begin, page_of(t_begin));
+  store_tile(0);
   int pg_nxt = page_of(t_begin + 1);
   __syncthreads();
 
@@ -413,6 +418,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
 //     Any order of the contraction over the head dim will do, so step 4 i + u takes word u of piece i: the values
 //     32 (2 i + hf) + 8 u .. + 7 of the row, and Q's rows are loaded in that order.
 //   * V needs transposing: its bf16 values go through rows in LDS that belong to the wave alone, without barriers.
+// Bound by memory: a token each behind 64 x 1-32 K cached (64/8 heads of 128) 226 us, 5.1 TB/s of codes and scales, above a
+// large copy's rate (321 us with branches around the loads and whole items, see few_rows_split for the cut).
 // ---------------------------------------------------------------------------------------------
 template <int D, int PAGE>
 __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __bf16* __restrict__ q,
@@ -489,7 +496,8 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
   const __bf16* vl[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
-    vl[db] = vs + (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) + 4 * (lane & 1);
+    vl[db] = vs + (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) +
+             4 * (lane & 1);
   f32x16 oacc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};

@@ -2,6 +2,7 @@
 #include "wavepp_q4.h"
 #include "internal.h"
 #include "plan.h"
+#include "q4.h"
 
 #include <exception>
 

@@ -1,6 +1,7 @@
 // Plans of the 4-bit cache and of linear attention over seeded random waves, host-only, under sanitizers: every item of an
 // accepted plan within its request, all of a request's tokens and keys covered once, in order.
 #include "lin_host.cpp"
+#include "q4.h"
 #include "wavepp_q4.h"
 
 #include <cstdio>
