@@ -12,6 +12,11 @@ constexpr int kLinBlock = 64;                // tokens per block of the chunkwis
 // eight tokens, 159 and 156 at twelve, 197 and 158 at sixteen; 4 of 32 of 128 x 64: 7.1 and 9.0, 8.9 and 9.2, 11.1 and 9.1.
 constexpr int kLinStepTokens = 10;
 
+// Heads of one workgroup of the blocks: two of 64 columns where they share q and k, whose products they then share too.
+constexpr int lin_heads(int num_heads, int num_qk_heads, int head_dim_v) {
+  return head_dim_v == 64 && num_heads / num_qk_heads % 2 == 0 ? 2 : 1;
+}
+
 struct alignas(16) LinHeader {
   uint32_t magic;
   uint32_t serial;

@@ -7,7 +7,7 @@
 //   O = scale (diag(lam) Q S0 + ((Q K^T) * D) V),      S = lam_64 S0 + K^T diag(D[64][.]) V.
 // All factors are products of decays, never quotients, so a decay of zero (or a tiny one) needs no special case.
 //
-// A workgroup runs one segment of one (request, head), block after block; wave w of its d_v / 16 owns the state's
+// A workgroup runs one segment of one (request, head), or of two heads, block after block; wave w of a head owns its state's
 // columns 16 w .. 16 w + 15 as 16 x 16 fp32 accumulator tiles.  The accumulator layout of v_mfma_f32_16x16x32_bf16 (lane =
 // column, four rows a lane) is that of an operand whose contraction runs over the rows of two tiles in a permuted
 // order, so the state feeds O^T = S0^T Q^T from registers, Q rows being read from LDS in that order; V and K^T
@@ -124,48 +124,58 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 }
 
 // ---------------------------------------------------------------------------------------------
-// Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.  Two blocks lie in LDS where d_v is
-// 128 (one workgroup of eight waves a CU), one where it is 64 (two of four waves: 207 -> 170 us on three ragged prompts, 32
-// heads of 128 x 64).
+// Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.  A workgroup has 128 columns: a head's,
+// or those of two heads of 64 that share q and k (HP = 2), whose rows of v and out lie side by side and whose Q K^T is one
+// product with two tables of decays (three ragged prompts, 32/8 heads of 128 x 64: 132 -> 125 us).  Two blocks lie in
+// LDS then, one workgroup of eight waves a CU; heads of 64 by themselves have one block and two workgroups of four waves (207 ->
+// 170 us on those prompts when it came in).
 // ---------------------------------------------------------------------------------------------
-template <int DK, int DV, bool AHEAD>
-__global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
+template <int DK, int DV, int HP, bool AHEAD>
+__global__ __launch_bounds__(DV * HP * 4, AHEAD && DV * HP == 128 ? 4 : 2) void lin_blocks_kernel(
     LinDevPlan p, const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
     const float* __restrict__ alpha, float* pool, __bf16* __restrict__ out) {
-  constexpr int NW = DV / 16, NT = NW * 64;
+  constexpr int COLS = DV * HP, NW = COLS / 16, NT = NW * 64;    // columns of the workgroup's heads, side by side
   // LDS layouts, for its 64 banks.  Q's and P's rows keep each 32 of their columns in the order of an operand's slots
   // (4-column group u of eight at place 2 (u % 4) + u / 4), so one 16-byte read gives an operand, eight rows on distinct
   // banks.  K, V: transposed reads of 8 rows x 32 bytes on distinct banks.  K's rows with bit 3 set have neighbouring
   // 16-byte pieces swapped, which puts the 8-byte reads of 16 rows on distinct banks too.
-  constexpr int QS = DK + 8, KS = DK + 16, VS = DV + 16, PS = kC + 8, GS = 20;
-  constexpr int KL = kC * DK / 8 / NT, VL = kC * DV / 8 / NT;     // 16-byte pieces per thread and block
+  constexpr int QS = DK + 8, KS = DK + 16, VS = COLS + 16, PS = kC + 8;
+  constexpr int KL = kC * DK / 8 / NT, VL = kC * COLS / 8 / NT;   // 16-byte pieces per thread and block
   constexpr int CT = DK / 16;                                     // row tiles of the state
-  constexpr int BUF = DV == 128 ? 2 : 1;                          // blocks in LDS
+  constexpr int BUF = COLS == 128 ? 2 : 1;                        // blocks in LDS
+  constexpr int DT = 160;                                         // a tile of D on the diagonal
+  struct alignas(16) Decays {
+    float run[3][kC];                  // [u][i]: alpha_{16 (u + 1)} ... alpha_i
+    float lam[kC];                     // scale alpha_0 ... alpha_i
+    float rest[kC], wt[kC];            // alpha after j: in its 16 times scale, in the block
+    float diag[AHEAD ? 4 : 4 * DT];    // D's 16 x 16 tiles on the diagonal, times scale, see diag_at
+  };
   struct alignas(16) Block {
     __bf16 q[AHEAD ? 8 : kC * QS];
     __bf16 k[kC * KS];
     __bf16 v[kC * VS];
-    float run[3][kC];                  // [u][i]: alpha_{16 (u + 1)} ... alpha_i
-    float lam[kC];                     // scale alpha_0 ... alpha_i
-    float rest[kC], wt[kC];            // alpha after j: in its 16 times scale, in the block
-    float diag[AHEAD ? 4 : kC * GS];   // D's 16 x 16 tiles on the diagonal, times scale
-    float gamma;                       // the block's decay
-    int bad[8];                        // per wave: a value of V is not finite
+    Decays d[HP];
+    float gamma[HP];                   // the block's decay
+    int bad[NW];                       // per wave, bit h: a value of V of head h is not finite
   };
   __shared__ __attribute__((aligned(16))) Block blk[BUF];
-  __shared__ __attribute__((aligned(16))) __bf16 pm[2][AHEAD ? 8 : kC * PS];   // scale (Q K^T) * D
+  __shared__ __attribute__((aligned(16))) __bf16 pm[2][HP][AHEAD ? 8 : kC * PS];   // scale (Q K^T) * D
+  // Where four columns of row l of a diagonal tile lie: only the quads that reach the diagonal are kept.
+  auto diag_at = [](int l, int quad) { return 4 * (2 * (l / 4) * (l / 4 + 1) + l % 4 * (l / 4 + 1) + quad); };
 
   if (!lin_meta_ok(p)) return;
   const int H = p.num_heads, Hqk = p.num_qk_heads;
   // Workgroups go round-robin to the kNumXcd L2 domains: the heads that share a q/k head read its rows through one.
-  const int G = H / Hqk, unit = blockIdx.x / (kNumXcd * G) * kNumXcd + blockIdx.x % kNumXcd;
+  const int G = H / Hqk / HP, unit = blockIdx.x / (kNumXcd * G) * kNumXcd + blockIdx.x % kNumXcd;
   if (unit >= (AHEAD ? p.num_ahead : p.num_segments) * Hqk) return;
   const LinItem it = item_at(p.segments + unit / Hqk);
-  const int qk_head = unit % Hqk, head = qk_head * G + blockIdx.x / kNumXcd % G;
+  const int qk_head = unit % Hqk, first = (qk_head * G + blockIdx.x / kNumXcd % G) * HP;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int mine = HP == 1 ? 0 : wave / (DV / 16), part = HP == 1 ? wave : wave % (DV / 16);   // of the heads; of the head
+  const int head = first + mine, col = 16 * part + l16;
 
-  f32x4 S[CT];                           // tile c, lane: rows 16 c + 4 g .. + 3 of column 16 wave + l16
+  f32x4 S[CT];                           // tile c, lane: rows 16 c + 4 g .. + 3 of column col
 #pragma unroll
   for (int c = 0; c < CT; ++c) S[c] = f32x4{};
   if (!AHEAD) {
@@ -173,12 +183,12 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 #pragma unroll
       for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[c][r] = s0[(16 * c + 4 * g + r) * DV + 16 * wave + l16];
+        for (int r = 0; r < 4; ++r) S[c][r] = s0[(16 * c + 4 * g + r) * DV + col];
     }
     // the tiles above the diagonal that the products with V run over
-    for (int i = tid; i < 2 * 32 * 16; i += NT) {
+    for (int i = tid; i < 2 * HP * 32 * 16; i += NT) {
       const int u = i % 512;
-      pm[i / 512][AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
+      pm[i / 512 % 2][i / 1024][AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
     }
   }
 
@@ -198,7 +208,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 #pragma unroll
   for (int i = 0; i < VL; ++i) {
     const int c = tid + NT * i;
-    v_off[i] = uint32_t(c / (DV / 8) * H * DV + c % (DV / 8) * 8) * 2;
+    v_off[i] = uint32_t(c / (COLS / 8) * H * DV + c % (COLS / 8) * 8) * 2;
   }
   const uint32_t a_row = p.alpha_per_token ? uint32_t(H) * 4 : 0;
   auto load = [&](Rows& x, int t0) {
@@ -206,7 +216,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     const int64_t tok = it.cu + min(t0, it.len);
     const auto qb = block_rows(q + (tok * Hqk + qk_head) * DK, rows * uint32_t(Hqk * DK * 2));
     const auto kb = block_rows(k + (tok * Hqk + qk_head) * DK, rows * uint32_t(Hqk * DK * 2));
-    const auto vb = block_rows(v + (tok * H + head) * DV, rows * uint32_t(H * DV * 2));
+    const auto vb = block_rows(v + (tok * H + first) * DV, rows * uint32_t(H * DV * 2));
     const auto ab = block_rows(alpha + (p.alpha_per_token ? tok * H + head : head), p.alpha_per_token ? rows * a_row : 4);
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
@@ -235,47 +245,50 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     }
 #pragma unroll
     for (int i = 0; i < VL; ++i) {
-      const int c = tid + NT * i, row = c / (DV / 8), at = c % (DV / 8) * 8;
+      const int c = tid + NT * i, row = c / (COLS / 8), at = c % (COLS / 8) * 8;
       *reinterpret_cast<u32x4*>(&b.v[row * VS + at]) = rows.v[i];
 #pragma unroll
       for (int u = 0; u < 4; ++u) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, rows.v[i][u] & 0x7FFF7FFFu));
     }
     if (!AHEAD) {
-      const bool bad = __any(max(top[0], top[1]) >= 0x7F80);
-      if (lane == 0) b.bad[wave] = bad;
+      const uint64_t bad = __ballot(max(top[0], top[1]) >= 0x7F80);      // of two heads, each second eight lanes have one
+      const uint64_t one = HP == 1 ? ~uint64_t(0) : 0x00FF00FF00FF00FFull;
+      if (lane == 0) b.bad[wave] = int((bad & one) != 0) | int((bad & ~one) != 0) << 1;
     }
     const float a = t0 + lane < it.len ? rows.a : 1.0f;    // no decay behind the last token
-    if (wave < 4) {
+    if (part < 4) {
+      Decays& d = b.d[mine];
       const float x = row_products(a);
       const float x0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 15));
       const float x1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 31));
       const float x2 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 47));
       const float x3 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63));
       float before = 1.0f;
-      if (g > 0 && wave <= 0) before *= x0;
-      if (g > 1 && wave <= 1) before *= x1;
-      if (g > 2 && wave <= 2) before *= x2;
-      if (wave > 0) b.run[wave - 1][lane] = before * x;
-      else b.lam[lane] = before * x * p.scale;
+      if (g > 0 && part <= 0) before *= x0;
+      if (g > 1 && part <= 1) before *= x1;
+      if (g > 2 && part <= 2) before *= x2;
+      if (part > 0) d.run[part - 1][lane] = before * x;
+      else d.lam[lane] = before * x * p.scale;
       const float all = x0 * x1 * x2 * x3;
       total *= all;
-      if (tid == 0) b.gamma = all;
-      if (wave == 1) {
+      if (part == 0 && lane == 0) b.gamma[mine] = all;
+      if (part == 1) {
         const float y = row_products_after(a);
-        b.rest[lane] = y * p.scale;
+        d.rest[lane] = y * p.scale;
         float after = 1.0f;
         if (g < 3) after *= x3;
         if (g < 2) after *= x2;
         if (g < 1) after *= x1;
-        b.wt[lane] = y * after;
+        d.wt[lane] = y * after;
       }
-      if (!AHEAD && wave == 2) {
-        float d[16];
-        row_table(a, l16, 0.0f, d);
+      if (!AHEAD && part == 2) {
+        float row[16];
+        row_table(a, l16, 0.0f, row);
 #pragma unroll
-        for (int j = 0; j < 16; j += 4)
-          *reinterpret_cast<f32x4*>(&b.diag[AHEAD ? 0 : lane * GS + j]) =
-              f32x4{d[j], d[j + 1], d[j + 2], d[j + 3]} * p.scale;
+        for (int u = 0; u < 4; ++u)
+          if (4 * u <= l16)
+            *reinterpret_cast<f32x4*>(&d.diag[AHEAD ? 0 : DT * g + diag_at(l16, u)]) =
+                f32x4{row[4 * u], row[4 * u + 1], row[4 * u + 2], row[4 * u + 3]} * p.scale;
       }
     }
   };
@@ -288,7 +301,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
   const uint32_t o_off = uint32_t(l16 * H * DV + 16 * wave + 4 * g) * 2;
   auto put = [&](int t0) {
     const int rows = __builtin_amdgcn_readfirstlane(min(kC, it.len - t0));
-    const auto ob = block_rows(out + (int64_t(it.cu + t0) * H + head) * DV, rows * uint32_t(H * DV * 2));
+    const auto ob = block_rows(out + (int64_t(it.cu + t0) * H + first) * DV, rows * uint32_t(H * DV * 2));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       bf16x4 x;
@@ -326,21 +339,24 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
           x = mfma(cat(*reinterpret_cast<const bf16x4*>(kr), *reinterpret_cast<const bf16x4*>(kr + 16)),
                    operand(b.q, (16 * ti + l16) * QS + 32 * s + 8 * g), x);
         }
-        bf16x4 y;
-        if (ti == tj) {                                    // above the diagonal nothing, whatever the product was
-          const f32x4 d = *reinterpret_cast<const f32x4*>(&b.diag[(16 * ti + l16) * GS + 4 * g]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(4 * g + e <= l16 ? x[e] * d[e] : 0.0f);
-        } else {
-          const f32x4 d = *reinterpret_cast<const f32x4*>(&b.rest[16 * tj + 4 * g]);
-          const float w = b.run[tj][16 * ti + l16];
+        for (int h = 0; h < HP; ++h) {
+          bf16x4 y;
+          if (ti == tj) {                                  // above the diagonal nothing, whatever the product was
+            const f32x4 d = *reinterpret_cast<const f32x4*>(&b.d[h].diag[DT * ti + diag_at(l16, min(g, l16 / 4))]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
+            for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(4 * g + e <= l16 ? x[e] * d[e] : 0.0f);
+          } else {
+            const f32x4 d = *reinterpret_cast<const f32x4*>(&b.d[h].rest[16 * tj + 4 * g]);
+            const float w = b.d[h].run[tj][16 * ti + l16];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = static_cast<__bf16>(x[e] * (d[e] * w));
+          }
+          *reinterpret_cast<bf16x4*>(&pm[half][h][(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
         }
-        *reinterpret_cast<bf16x4*>(&pm[half][(16 * ti + l16) * PS + tj / 2 * 32 + 8 * g + tj % 2 * 4]) = y;
       }
     }
-    if (pending) finish(pm[half ^ 1], t0 - kC);
+    if (pending) finish(pm[half ^ 1][mine], t0 - kC);
     if constexpr (!AHEAD) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] = f32x4{};
@@ -352,7 +368,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float l = b.lam[16 * i + l16];
+        const float l = b.d[mine].lam[16 * i + l16];
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][e] *= l;
       }
@@ -362,7 +378,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 #pragma unroll
     for (int t = 0; t < 2; ++t) vf[t] = cat(lds_read_tr(vl + 32 * t * VS), lds_read_tr(vl + (32 * t + 16) * VS));
     // S = lam_64 S + K^T (w V): the weighted values as three bf16 parts, 24 bits, so that the state is as exact as in fp32
-    const float gamma = b.gamma;
+    const float gamma = b.gamma[mine];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
@@ -370,8 +386,8 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
     const __bf16* kl = &b.k[(4 * g + (l16 >> 2)) * KS + ((4 * (l16 & 3)) ^ (4 * g & 8))];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 4 * g]);
-      const f32x4 w1 = *reinterpret_cast<const f32x4*>(&b.wt[32 * t + 16 + 4 * g]);
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(&b.d[mine].wt[32 * t + 4 * g]);
+      const f32x4 w1 = *reinterpret_cast<const f32x4*>(&b.d[mine].wt[32 * t + 16 + 4 * g]);
       u32x4 hi, mid, lo;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
@@ -397,13 +413,14 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
       for (int w = 0; w < NW; ++w) any |= b.bad[w];
       // A value of V that is not finite, times the zeros above the diagonal, would reach the tokens before it: such a
       // block's weights and values are summed pair by pair.
-      if (__builtin_amdgcn_readfirstlane(any)) {
-        __syncthreads();                 // P is whole
+      any = __builtin_amdgcn_readfirstlane(any);
+      if (any) __syncthreads();          // P is whole
+      if (any >> mine & 1) {
         for (int j = 0; j < kC; ++j) {
           const bf16x4 x = *reinterpret_cast<const bf16x4*>(&b.v[j * VS + 16 * wave + 4 * g]);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float w = float(pm[half][(16 * i + l16) * PS + j / 32 * 32 + j / 4 % 4 * 8 + j / 16 % 2 * 4 + j % 4]);
+            const float w = float(pm[half][mine][(16 * i + l16) * PS + j / 32 * 32 + j / 4 % 4 * 8 + j / 16 % 2 * 4 + j % 4]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[i][e] = j <= 16 * i + l16 ? fmaf(w, float(x[e]), o[i][e]) : o[i][e];
           }
@@ -419,7 +436,7 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
   }
   if (pending) {
     const int blocks = (it.len + kC - 1) / kC;
-    finish(pm[(blocks - 1) & 1], (blocks - 1) * kC);
+    finish(pm[(blocks - 1) & 1][mine], (blocks - 1) * kC);
   }
 
   const int64_t size = int64_t(DK) * DV;
@@ -429,9 +446,9 @@ __global__ __launch_bounds__(DV * 4, 2) void lin_blocks_kernel(
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[(16 * c + 4 * g + r) * DV + 16 * wave + l16] = S[c][r];
+      for (int r = 0; r < 4; ++r) to[(16 * c + 4 * g + r) * DV + col] = S[c][r];
   }
-  if (AHEAD && tid == 0) p.part_decay[int64_t(it.part_out) * H + head] = total;
+  if (AHEAD && part == 0 && lane == 0) p.part_decay[int64_t(it.part_out) * H + head] = total;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -515,25 +532,31 @@ __global__ __launch_bounds__(256) void lin_step_kernel(LinDevPlan p, const __bf1
   for (int i = 0; i < RPT; ++i) *reinterpret_cast<f32x4*>(to + (rg + RG * i) * DV + at) = S[i];
 }
 
+template <int DK, int DV, int HP>
+void launch_blocks(const LinDevPlan& p, const __bf16* q, const __bf16* k, const __bf16* v, const float* alpha, float* pool,
+                   __bf16* out, hipStream_t stream) {
+  // a workgroup for every segment and HP heads, the segments' q/k heads padded to whole rounds of the L2 domains
+  auto grid = [&](int segments) {
+    return dim3((segments * p.num_qk_heads + kNumXcd - 1) / kNumXcd * kNumXcd * (p.num_heads / p.num_qk_heads / HP));
+  };
+  if (p.num_ahead)
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, HP, true>), grid(p.num_ahead), dim3(4 * DV * HP), 0, stream, p, q, k, v,
+                       alpha, pool, out);
+  if (p.num_scans)
+    hipLaunchKernelGGL(lin_scan_kernel, dim3(p.num_scans * p.num_heads, DK * DV / 1024), dim3(256), 0, stream, p, pool);
+  if (p.num_segments)
+    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, HP, false>), grid(p.num_segments), dim3(4 * DV * HP), 0, stream, p, q, k,
+                       v, alpha, pool, out);
+}
+
 template <int DK, int DV>
 hipError_t launch_dims(const LinDevPlan& p, const __bf16* q, const __bf16* k, const __bf16* v, const float* alpha,
                        float* pool, __bf16* out, hipStream_t stream) {
-  const int H = p.num_heads;
-  // a workgroup for every (segment, head), the segments' q/k heads padded to whole rounds of the L2 domains
-  auto grid = [&](int segments) {
-    return dim3((segments * p.num_qk_heads + kNumXcd - 1) / kNumXcd * kNumXcd * (H / p.num_qk_heads));
-  };
   if (p.num_steps)
-    hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(p.num_steps * H * (DV / 32)), dim3(256), 0, stream, p, q, k, v, alpha,
-                       pool, out);
-  if (p.num_ahead)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, true>), grid(p.num_ahead), dim3(4 * DV), 0, stream, p, q, k, v, alpha,
-                       pool, out);
-  if (p.num_scans)
-    hipLaunchKernelGGL(lin_scan_kernel, dim3(p.num_scans * H, DK * DV / 1024), dim3(256), 0, stream, p, pool);
-  if (p.num_segments)
-    hipLaunchKernelGGL((lin_blocks_kernel<DK, DV, false>), grid(p.num_segments), dim3(4 * DV), 0, stream, p, q, k, v,
-                       alpha, pool, out);
+    hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(p.num_steps * p.num_heads * (DV / 32)), dim3(256), 0, stream, p, q, k,
+                       v, alpha, pool, out);
+  if (lin_heads(p.num_heads, p.num_qk_heads, DV) == 2) launch_blocks<DK, DV, DV == 64 ? 2 : 1>(p, q, k, v, alpha, pool, out, stream);
+  else launch_blocks<DK, DV, 1>(p, q, k, v, alpha, pool, out, stream);
   return hipGetLastError();
 }
 

@@ -90,7 +90,7 @@ def check(args, t, g, what="", finite=None):
 
 
 @pytest.mark.parametrize("dk,dv", DIMS)
-@pytest.mark.parametrize("H,Hqk", [(4, 4), (6, 2), (5, 1)])
+@pytest.mark.parametrize("H,Hqk", [(4, 4), (6, 2), (5, 1), (8, 2)])
 @pytest.mark.parametrize("per_token", [True, False])
 def test_chunks_of_all_lengths(dk, dv, H, Hqk, per_token):
     lens = [1, 63, 0, 64, 65, 2, 10, 11, 130, 200, 1]
@@ -173,6 +173,21 @@ def test_tokens_before_a_bad_number_are_as_without_it(name, bad):
     assert (np.abs(x - y) <= 2.2 * 2.0 ** -7 * size).all()
     gone = b["out"].float().cpu().numpy()[[75, 203, 290]]
     assert not np.isfinite(gone).any()
+
+
+@pytest.mark.parametrize("dv", [64, 128])
+def test_a_bad_number_of_one_head_leaves_the_others_alone(dv):
+    """Heads that share q and k: a value or a decay of one that is not finite changes no bit of another's."""
+    args, t = make([200, 9, 90], [-1, 0, 1], [2, 3, 1], 4, 2, 128, dv, seed=54)
+    a = on_gpu(args, t)
+    for name, head in (("v", 0), ("v", 3), ("alpha", 1), ("alpha", 2)):
+        spoiled = {n: x.clone() for n, x in t.items()}
+        for at in (3, 75, 203, 290):
+            spoiled[name][at, head] = float("nan") if at != 75 else float("inf")
+        b = on_gpu(args, spoiled)
+        rest = [h for h in range(4) if h != head]
+        assert same(a["out"][:, rest], b["out"][:, rest]) and same(a["state_pool"][:, rest], b["state_pool"][:, rest])
+        assert not torch.isfinite(b["out"][75, head].float()).any()
 
 
 def test_repeated_calls_are_bit_identical_and_stale_workspaces_write_nothing():
