@@ -188,7 +188,8 @@ __global__ __launch_bounds__(DV * HP * 4, AHEAD && DV * HP == 128 ? 4 : 2) void 
     // the tiles above the diagonal that the products with V run over
     for (int i = tid; i < 2 * HP * 32 * 16; i += NT) {
       const int u = i % 512;
-      pm[i / 512 % 2][i / 1024][AHEAD ? 0 : (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4] = __bf16(0.0f);
+      const int at = (u / 256 * 32 + u / 16 % 16) * PS + u / 256 * 32 + u / 4 % 4 * 8 + 4 + u % 4;
+      pm[i / 512 % 2][i / 1024][AHEAD ? 0 : at] = __bf16(0.0f);
     }
   }
 
@@ -555,8 +556,10 @@ hipError_t launch_dims(const LinDevPlan& p, const __bf16* q, const __bf16* k, co
   if (p.num_steps)
     hipLaunchKernelGGL((lin_step_kernel<DK, DV>), dim3(p.num_steps * p.num_heads * (DV / 32)), dim3(256), 0, stream, p, q, k,
                        v, alpha, pool, out);
-  if (lin_heads(p.num_heads, p.num_qk_heads, DV) == 2) launch_blocks<DK, DV, DV == 64 ? 2 : 1>(p, q, k, v, alpha, pool, out, stream);
-  else launch_blocks<DK, DV, 1>(p, q, k, v, alpha, pool, out, stream);
+  if (DV == 64 && lin_heads(p.num_heads, p.num_qk_heads, DV) == 2)
+    launch_blocks<DK, DV, DV == 64 ? 2 : 1>(p, q, k, v, alpha, pool, out, stream);
+  else
+    launch_blocks<DK, DV, 1>(p, q, k, v, alpha, pool, out, stream);
   return hipGetLastError();
 }
 
