@@ -62,8 +62,9 @@ int wavepp_q4_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
 
 /* Attention of the wave's queries over the cached values, as defined in wavepp_attn.h with K and V read
  * from 4-bit pages: bf16 q and out, fp32 natural-log lse (or NULL).  bf16 products of the exact cached
- * values with fp32 accumulation and softmax.  Deterministic: repeated calls give bit-identical
- * results.  Errors as for wavepp_attn_chunked_prefill. */
+ * values with fp32 accumulation and softmax.  A row whose softmax sum is not a number (a NaN in its query, a logit
+ * that overflows upwards) has NaN as its lse, whole or joined from splits; -infinity says that no key had any weight.
+ * Deterministic: repeated calls give bit-identical results.  Errors as for wavepp_attn_chunked_prefill. */
 int wavepp_q4_chunked_prefill(const wavepp_plan* plan, const void* q, const void* k_pool, const void* v_pool, void* out,
                               float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);
 

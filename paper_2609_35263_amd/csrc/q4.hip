@@ -379,9 +379,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
   }
 
   // ---- epilogue: O = O^T / l, lse = ln(l) + m (natural log) ------------------------------------
+  // A sum of zero saw no weight; one that is not a number stays so in the LSE, and so in those that it is merged with.
   if (!row_ok) return;
-  const float inv_l = l_run > 0.0f ? 1.0f / l_run : 0.0f;
-  const float lse_v = l_run > 0.0f ? (m_run + __log2f(l_run)) * kLn2 : -INFINITY;
+  const float inv_l = l_run == 0.0f ? 0.0f : 1.0f / l_run;
+  const float lse_v = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * kLn2;
   if (it.part < 0) {
     __bf16* orow = out + (int64_t(rm.cu + tok) * Hq + head) * D;
 #pragma unroll
@@ -602,9 +603,9 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
 #pragma unroll
   for (int w = 0; w < 4; ++w) rm_ = fmaxf(rm_, wave_m[w][row]);
 #pragma unroll
-  for (int w = 0; w < 4; ++w) l += wave_m[w][row] == -INFINITY ? 0.0f : wave_l[w][row] * fast_exp2(wave_m[w][row] - rm_);
-  const float inv_l = l > 0.0f ? 1.0f / l : 0.0f;
-  const float lse_v = l > 0.0f ? (rm_ + __log2f(l)) * kLn2 : -INFINITY;
+  for (int w = 0; w < 4; ++w) l += wave_l[w][row] == 0.0f ? 0.0f : wave_l[w][row] * fast_exp2(wave_m[w][row] - rm_);
+  const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;       // as in the kernel above
+  const float lse_v = l == 0.0f ? -INFINITY : (rm_ + __log2f(l)) * kLn2;
   const int orow_t = it.row0 + row, otok = orow_t / G;
   const int64_t orow = int64_t(rm.cu + otok) * Hq + it.kv_head * G + (orow_t - otok * G);
 #pragma unroll
