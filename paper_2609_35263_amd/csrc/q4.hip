@@ -163,6 +163,14 @@ __global__ __launch_bounds__(256) void q4_read_kernel(DevPlan p, const uint8_t* 
   }
 }
 
+// The sum that a row's outputs are divided by: 0 for a row of no weight, NaN for one that has no sum.  The key that set the
+// reference m (a logit times log2 e) has a weight of 2^d, d being what m lost when it was rounded: nothing that matters up
+// to 2^28, where it is 16 at most and the sum takes it out again; beyond, the weight may be anything, 0 and infinity among it.
+__device__ __forceinline__ float row_sum(float m, float l) {
+  if (m == -INFINITY && l == 0.0f) return 0.0f;
+  return fabsf(m) <= 0x1p28f ? l : NAN;
+}
+
 // ---------------------------------------------------------------------------------------------
 // Attention of many rows.  The layout is that of the kernel over bf16 pages (kernels.hip): a workgroup of NW waves
 // takes 32 NW query rows of one (request, KV head) and walks tiles of keys that all its rows share; logits S^T = K Q^T
@@ -379,10 +387,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
   }
 
   // ---- epilogue: O = O^T / l, lse = ln(l) + m (natural log) ------------------------------------
-  // A sum of zero saw no weight; one that is not a number stays so in the LSE, and so in those that it is merged with.
   if (!row_ok) return;
-  const float inv_l = l_run == 0.0f ? 0.0f : 1.0f / l_run;
-  const float lse_v = l_run == 0.0f ? -INFINITY : (m_run + __log2f(l_run)) * kLn2;
+  const float sum = row_sum(m_run, l_run);
+  const float inv_l = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float lse_v = sum == 0.0f ? -INFINITY : (m_run + __log2f(sum)) * kLn2;
   if (it.part < 0) {
     __bf16* orow = out + (int64_t(rm.cu + tok) * Hq + head) * D;
 #pragma unroll
@@ -604,7 +612,8 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
   for (int w = 0; w < 4; ++w) rm_ = fmaxf(rm_, wave_m[w][row]);
 #pragma unroll
   for (int w = 0; w < 4; ++w) l += wave_l[w][row] == 0.0f ? 0.0f : wave_l[w][row] * fast_exp2(wave_m[w][row] - rm_);
-  const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;       // as in the kernel above
+  l = row_sum(rm_, l);
+  const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
   const float lse_v = l == 0.0f ? -INFINITY : (rm_ + __log2f(l)) * kLn2;
   const int orow_t = it.row0 + row, otok = orow_t / G;
   const int64_t orow = int64_t(rm.cu + otok) * Hq + it.kv_head * G + (orow_t - otok * G);

@@ -9,8 +9,9 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 import workloads as wl
-from tests.test_gpu_q4 import make, on_gpu, same
+from tests.test_gpu_q4 import LSE, MERGED, make, on_gpu, same
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +72,29 @@ def test_a_row_whose_keys_all_weigh_nothing_still_says_so():
     t["q"], t["k_new"] = -t["q"].abs(), torch.full_like(t["k_new"], float("inf"))
     g = on_gpu(spec, t)
     assert (g["lse"] == -float("inf")).all()
+
+
+@pytest.mark.parametrize("name", sorted(WAVES))
+@pytest.mark.parametrize("splits", [0, 3])
+def test_one_bad_number_of_a_key_with_a_finite_logit(name, splits):
+    """A logit of order 1e37 is finite, but fp32 cannot place its exponential: where it is the largest, out and LSE are NaN.
+    Where it is as far below zero the key weighs nothing, as it should."""
+    def spoil(sign):
+        def do(t):
+            t["k_new"][0, :, 5] = float("nan")       # cached as 6 * 2^125, the rest of its block as zeros
+            c = WAVES[name][5][0]
+            t["q"][:c, :, 5] = (sign * (0.25 + 0.5 * torch.rand(t["q"][:c, :, 5].shape, generator=gen))).to(torch.bfloat16)
+        return do
+
+    gen = torch.Generator().manual_seed(75)
+    check(*run(name, splits, spoil(1.0)))
+    clean, g, seen = run(name, splits, spoil(-1.0))
+    assert same(clean["out"][~seen], g["out"][~seen]) and same(clean["lse"][~seen], g["lse"][~seen])
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=71, name=name)
+    k, v = (oracle.q4.pool_values(g[n].cpu().numpy(), dim, page) for n in ("k_pool", "v_pool"))
+    with np.errstate(over="ignore", invalid="ignore"):
+        o, lse, size = oracle.q4.attention(wl.to_bits(g["q"].cpu()), k, v, spec.prefix_lens, spec.chunk_lens, spec.block_table, page,
+                                           spec.softmax_scale)
+    assert (np.abs(g["out"].float().cpu().numpy() - o) <= MERGED * size).all()
+    assert (np.abs(g["lse"].cpu().numpy() - lse) <= LSE).all()
