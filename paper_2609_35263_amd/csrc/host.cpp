@@ -42,7 +42,11 @@ int set_error(int status, const char* fmt, ...) {
   va_start(ap, fmt);
   vsnprintf(buf, sizeof(buf), fmt, ap);
   va_end(ap);
-  g_last_error = buf;
+  try {
+    g_last_error = buf;
+  } catch (const std::exception&) {        // no memory for the detail
+    g_last_error.clear();
+  }
   return status;
 }
 
@@ -64,11 +68,6 @@ namespace {
 std::mutex g_ws_mu;
 std::unordered_map<uintptr_t, uint32_t> g_ws_serial;
 }  // namespace
-
-void note_upload(const void* workspace, uint32_t serial) {
-  std::lock_guard<std::mutex> lock(g_ws_mu);
-  g_ws_serial[reinterpret_cast<uintptr_t>(workspace)] = serial;
-}
 
 int require_upload(const void* workspace, uint32_t serial, const char* upload_fn) {
   uint32_t have = 0;
@@ -626,6 +625,16 @@ int stage_and_copy(const void* src, size_t bytes, void* dst, hipStream_t stream)
   return WAVEPP_OK;
 }
 
+int upload_plan(const void* blob, size_t bytes, uint32_t serial, void* workspace, hipStream_t stream) {
+  return guarded([&] {
+    const int st = stage_and_copy(blob, bytes, workspace, stream);
+    if (st) return st;
+    std::lock_guard<std::mutex> lock(g_ws_mu);
+    g_ws_serial[reinterpret_cast<uintptr_t>(workspace)] = serial;
+    return int(WAVEPP_OK);
+  });
+}
+
 }  // namespace wavepp
 
 namespace wavepp {
@@ -1022,7 +1031,7 @@ const char* wavepp_last_error(void) { return last_error_text(); }
 
 int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits,
                      wavepp_plan** out) {
-  return plan_wave(shape, batch, max_splits, false, out);
+  return guarded([&] { return plan_wave(shape, batch, max_splits, false, out); });
 }
 
 size_t wavepp_plan_workspace_bytes(const wavepp_plan* plan) { return plan ? plan->workspace_bytes : 0; }
@@ -1058,10 +1067,7 @@ int wavepp_attn_plan_upload(const wavepp_plan* plan, void* workspace, size_t ws_
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
   int st = check_workspace(plan, workspace, ws_bytes);
   if (st) return st;
-  st = stage_and_copy(plan->blob.data(), plan->blob.size(), workspace, stream);
-  if (st) return st;
-  note_upload(workspace, plan->serial);
-  return WAVEPP_OK;
+  return upload_plan(plan->blob.data(), plan->blob.size(), plan->serial, workspace, stream);
 }
 
 int wavepp_attn_append_kv(const wavepp_plan* plan, const void* k_new, const void* v_new, void* k_pool, void* v_pool,

@@ -2,8 +2,12 @@
 // Not part of the public ABI.
 #pragma once
 
+#include "wavepp_attn.h"
+
 #include <stdint.h>
 #include <hip/hip_runtime_api.h>
+
+#include <exception>
 
 namespace wavepp {
 
@@ -129,13 +133,21 @@ int set_error(int status, const char* fmt, ...);
 int set_hip_error(hipError_t e, const char* what);
 void clear_error();
 const char* last_error_text();
-int stage_and_copy(const void* src, size_t bytes, void* dst, hipStream_t stream);
 uint32_t next_serial();
-// Record that `workspace` was given the metadata of the plan with this serial (on the caller's
-// stream); require_upload returns WAVEPP_EINVAL, with a last-error message naming upload_fn, when
+// Copy a plan's metadata into `workspace` on the caller's stream and record that `workspace` was given the plan with this
+// serial; require_upload returns WAVEPP_EINVAL, with a last-error message naming upload_fn, when
 // the last upload into `workspace` was of another plan or there was none.
-void note_upload(const void* workspace, uint32_t serial);
+int upload_plan(const void* blob, size_t bytes, uint32_t serial, void* workspace, hipStream_t stream);
 int require_upload(const void* workspace, uint32_t serial, const char* upload_fn);
+// What an entry point does that allocates on the host: its C caller gets a status where an allocation fails.
+template <typename F>
+int guarded(F&& work) {
+  try {
+    return work();
+  } catch (const std::exception&) {
+    return set_error(WAVEPP_EINVAL, "out of host memory");
+  }
+}
 
 hipError_t launch_append(const DevPlan& p, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                          hipStream_t stream);

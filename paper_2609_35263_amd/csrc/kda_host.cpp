@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cstring>
+#include <memory>
 #include <new>
 #include <numeric>
 #include <vector>
@@ -107,11 +108,7 @@ std::vector<int32_t> chain_owners(const std::vector<KdaItem>& items, int heads) 
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-}  // namespace
-
-extern "C" {
-
-int wavepp_kda_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch, wavepp_kda_plan_t** out) {
+int make_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch, wavepp_kda_plan_t** out) {
   clear_error();
   if (!shape || !batch || !out) return set_error(WAVEPP_EINVAL, "null argument");
   *out = nullptr;
@@ -153,7 +150,7 @@ int wavepp_kda_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch
       return set_error(WAVEPP_EALIAS, "request %d resumes from slot %d, which request %d writes", r, si, writer[si]);
   }
 
-  auto plan = new (std::nothrow) wavepp_kda_plan_t();
+  std::unique_ptr<wavepp_kda_plan_t> plan(new (std::nothrow) wavepp_kda_plan_t());
   if (!plan) return set_error(WAVEPP_EINVAL, "out of host memory");
   plan->shape = s;
   plan->total_tokens = total;
@@ -175,10 +172,7 @@ int wavepp_kda_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch
   // longest chunks first: the order in which chains are given to workgroups
   std::stable_sort(plan->items.begin(), plan->items.end(),
                    [](const KdaItem& a, const KdaItem& b) { return a.len > b.len; });
-  if (int64_t(plan->items.size()) * s.num_heads > INT32_MAX / 2) {
-    delete plan;
-    return set_error(WAVEPP_EINVAL, "too many workgroups");
-  }
+  if (int64_t(plan->items.size()) * s.num_heads > INT32_MAX / 2) return set_error(WAVEPP_EINVAL, "too many workgroups");
   plan->off_items = align_up(sizeof(KdaHeader), 16);
   size_t bytes = plan->off_items + sizeof(KdaItem) * plan->items.size();
   std::vector<int32_t> list;
@@ -209,8 +203,16 @@ int wavepp_kda_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch
     memcpy(plan->blob.data() + plan->off_items + sizeof(KdaItem) * plan->items.size(), list.data(),
            sizeof(int32_t) * list.size());
   plan->workspace_bytes = align_up(plan->blob.size(), 256);
-  *out = plan;
+  *out = plan.release();
   return WAVEPP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int wavepp_kda_plan(const wavepp_kda_shape* shape, const wavepp_kda_batch* batch, wavepp_kda_plan_t** out) {
+  return guarded([&] { return make_plan(shape, batch, out); });
 }
 
 size_t wavepp_kda_workspace_bytes(const wavepp_kda_plan_t* plan) { return plan ? plan->workspace_bytes : 0; }
@@ -230,10 +232,7 @@ int wavepp_kda_upload(const wavepp_kda_plan_t* plan, void* workspace, size_t ws_
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
   int st = check_ws(plan, workspace, ws_bytes);
   if (st) return st;
-  st = stage_and_copy(plan->blob.data(), plan->blob.size(), workspace, stream);
-  if (st) return st;
-  note_upload(workspace, plan->serial);
-  return WAVEPP_OK;
+  return upload_plan(plan->blob.data(), plan->blob.size(), plan->serial, workspace, stream);
 }
 
 int wavepp_kda_chunked_prefill(const wavepp_kda_plan_t* plan, const void* q, const void* k, const void* v,

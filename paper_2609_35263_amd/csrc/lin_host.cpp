@@ -10,7 +10,6 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <exception>
 #include <functional>
 #include <memory>
 #include <new>
@@ -256,11 +255,7 @@ int make_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wave
 extern "C" {
 
 int wavepp_lin_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wavepp_lin_plan_t** out) {
-  try {
-    return make_plan(shape, batch, out);
-  } catch (const std::exception&) {
-    return set_error(WAVEPP_EINVAL, "out of host memory");
-  }
+  return guarded([&] { return make_plan(shape, batch, out); });
 }
 
 size_t wavepp_lin_workspace_bytes(const wavepp_lin_plan_t* plan) { return plan ? plan->workspace_bytes : 0; }
@@ -282,10 +277,7 @@ int wavepp_lin_upload(const wavepp_lin_plan_t* plan, void* workspace, size_t ws_
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
   int st = check_ws(plan, workspace, ws_bytes);
   if (st) return st;
-  st = stage_and_copy(plan->blob.data(), plan->blob.size(), workspace, stream);
-  if (st) return st;
-  note_upload(workspace, plan->serial);
-  return WAVEPP_OK;
+  return upload_plan(plan->blob.data(), plan->blob.size(), plan->serial, workspace, stream);
 }
 
 int wavepp_lin_chunked_prefill(const wavepp_lin_plan_t* plan, const void* q, const void* k, const void* v,

@@ -4,8 +4,6 @@
 #include "plan.h"
 #include "q4.h"
 
-#include <exception>
-
 using namespace wavepp;
 
 namespace {
@@ -41,11 +39,7 @@ size_t wavepp_q4_page_bytes(int32_t head_dim, int32_t page_size) {
 }
 
 int wavepp_q4_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, wavepp_plan** out) {
-  try {
-    return plan_wave(shape, batch, max_splits, true, out);
-  } catch (const std::exception&) {
-    return set_error(WAVEPP_EINVAL, "out of host memory");
-  }
+  return guarded([&] { return plan_wave(shape, batch, max_splits, true, out); });
 }
 
 int wavepp_q4_append_kv(const wavepp_plan* plan, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
