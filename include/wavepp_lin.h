@@ -73,8 +73,8 @@ typedef struct {
 } wavepp_lin_info;
 
 /* Validate the wave and build its work list; where it has fewer chains (request, head) than the chip has room
- * for, long chunks are cut into segments: each segment's own state first, then the states between them,
- * then all outputs at once.  Host only.  Errors as for wavepp_kda_plan. */
+ * for, or a chunk so long that it would run on after the others, long chunks are cut into segments: each segment's own
+ * state first, then the states between them, then all outputs at once.  Host only.  Errors as for wavepp_kda_plan. */
 int wavepp_lin_plan(const wavepp_lin_shape* shape, const wavepp_lin_batch* batch, wavepp_lin_plan_t** out);
 
 /* Device workspace the plan needs (metadata and partial states), 256-byte aligned. */
