@@ -126,9 +126,9 @@ __device__ __forceinline__ const float* start_of(const LinDevPlan& p, const LinI
 // ---------------------------------------------------------------------------------------------
 // Blocks of 64 tokens.  AHEAD: only the segment's own state, from zero, and its decay.  A workgroup has 128 columns: a head's,
 // or those of two heads of 64 that share q and k (HP = 2), whose rows of v and out lie side by side and whose Q K^T is one
-// product with two tables of decays (three ragged prompts, 32/8 heads of 128 x 64: 132 -> 125 us).  Two blocks lie in
-// LDS then, one workgroup of eight waves a CU; heads of 64 by themselves have one block and two workgroups of four waves (207 ->
-// 170 us on those prompts when it came in).
+// product with two tables of decays (three ragged prompts, 32/8 heads of 128 x 64: 132 -> 124 us, 119 -> 118 with the inputs
+// in a cache).  Two blocks lie in LDS then, one workgroup of eight waves a CU; heads of 64 by themselves have one block and two
+// workgroups of four waves (207 -> 170 us on those prompts when it came in).
 // ---------------------------------------------------------------------------------------------
 template <int DK, int DV, int HP, bool AHEAD>
 __global__ __launch_bounds__(DV * HP * 4, AHEAD && DV * HP == 128 ? 4 : 2) void lin_blocks_kernel(

@@ -39,6 +39,8 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // memory's time for a block of 128 + 128 columns.  Measured over forced cuts of seven waves (us, forced best / chosen):
 // 32 heads of 128 x 64, one by one, 4,627 + 4,948 + 6,968 tokens: 390 whole, 128 / 128; 64 of 128 x 128, 16,384 tokens: 912
 // whole, 380 / 380; 16 of 64 x 64, 2 x 8,000: 329 whole, 55 / 55; 8 of 128 x 128, 16,384: 798 whole, 70 / 70.
+// All with a head a workgroup: the two heads of a paired workgroup are modelled as two chains on a slot each, which was not
+// measured over forced cuts, and three workgroups of 64 x 64 heads fit on a CU where the model has two.
 constexpr double kMainOverhead = 3.0, kAheadOverhead = 2.0, kAheadBlock = 0.5, kScanBase = 1.5, kScanBlock = 0.01;
 constexpr double kMemoryBlock = 0.0046;
 

@@ -178,7 +178,7 @@ __device__ __forceinline__ float row_sum(float m, float l) {
 // straight from the accumulators.  A tile's codes are loaded (a quarter of the bytes, 8 registers a thread) before
 // the MFMAs of the tile before it and turned into bf16 rows in the other LDS buffer after them: once for all NW waves.
 // It is bound by the matrix instructions and the softmax's VALU work beside them, as over bf16 pages: 1,024 tokens behind 65,536
-// (64/8 heads of 128) 1,834 us, 1.22 PFLOP/s where a large library product reaches 1.34 (1,885 us with V's pieces in order,
+// (64/8 heads of 128) 1,834 us, 1.21 PFLOP/s where a large library product reaches 1.35 (1,885 us with V's pieces in order,
 // see v_place).  8 x 16 tokens behind 16-32 K: 136 us, four waves, twice the dequantisation for a row; the memory would
 // take 48.
 // ---------------------------------------------------------------------------------------------
@@ -427,8 +427,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
 //     Any order of the contraction over the head dim will do, so step 4 i + u takes word u of piece i: the values
 //     32 (2 i + hf) + 8 u .. + 7 of the row, and Q's rows are loaded in that order.
 //   * V needs transposing: its bf16 values go through rows in LDS that belong to the wave alone, without barriers.
-// Bound by memory: a token each behind 64 x 1-32 K cached (64/8 heads of 128) 226 us, 5.1 TB/s of codes and scales, above a
-// large copy's rate (321 us with branches around the loads and whole items, see few_rows_split for the cut).
+// Bound by memory: a token each behind 64 x 1-32 K cached (64/8 heads of 128, pages of 64) 226 us, 5.1 TB/s of codes and
+// scales, above a large copy's rate (321 us with branches around the loads and whole items, see few_rows_split for the cut).
+// With pages of 16 the same wave takes 280 us: at head dim 128 that form has 10 registers too many, and what it reads back
+// from scratch waits for both blocks in flight (28 bytes a lane; the form with pages of 64 has 254 registers and none).
 // ---------------------------------------------------------------------------------------------
 template <int D, int PAGE>
 __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __bf16* __restrict__ q,
@@ -576,7 +578,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
   };
 
   // Two blocks are in flight.  Loads are not branched around (a last block is loaded again instead), so the compiler
-  // knows their number and waits for the older block alone.
+  // knows their number and waits for the older block alone (but for the form that spills, see above).
   const int end = (it.kv_end + 31) / 32;
   int block = it.kv_begin / 32 + wave;
   if (block < end) {
