@@ -16,7 +16,7 @@
  * times s, ties to the even code, magnitudes over 6 s to 6 s; so with e inside its clamps no value is
  * off by more than s.  The format has no infinities and no NaN: they count as the largest finite
  * magnitude of their sign and reach only the queries that see their row.  A V row that had one shows there as
- * outputs of order 1e38 times its weight.  A K row that had one shows as NaN in outputs and LSE where it makes a
+ * outputs of order 1e38 times its weight, or infinite.  A K row that had one shows as NaN in outputs and LSE where it makes a
  * logit too large, and has no weight, so leaves no trace, where it makes it as far below zero.
  * Every value that the append stores is exactly a bf16 number.
  *
@@ -66,7 +66,8 @@ int wavepp_q4_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
  * from 4-bit pages: bf16 q and out, fp32 natural-log lse (or NULL).  bf16 products of the exact cached
  * values with fp32 accumulation and softmax.  A row whose softmax sum is not a number (a NaN in its query, a largest
  * logit that overflows or lies beyond 2^28 ln 2, where fp32 cannot place its exponential) has NaN as its output and
- * its lse, whole or joined from splits; an lse of -infinity says that no key had any weight.
+ * its lse, whole or joined from splits.  Logits under -2^28 ln 2 have no weight; an lse of -infinity says that no key
+ * had any, and the output then says nothing.
  * Deterministic: repeated calls give bit-identical results.  Errors as for wavepp_attn_chunked_prefill. */
 int wavepp_q4_chunked_prefill(const wavepp_plan* plan, const void* q, const void* k_pool, const void* v_pool, void* out,
                               float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);

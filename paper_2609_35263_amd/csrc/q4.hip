@@ -163,13 +163,14 @@ __global__ __launch_bounds__(256) void q4_read_kernel(DevPlan p, const uint8_t* 
   }
 }
 
-// The sum that a row's outputs are divided by: 0 for a row of no weight, NaN for one that has no sum.  The key that set the
-// reference m (a logit times log2 e) has a weight of 2^d, d being what m lost when it was rounded: nothing that matters up
-// to 2^28, where it is 16 at most and the sum takes it out again; beyond, the weight may be anything, 0 and infinity among it.
-__device__ __forceinline__ float row_sum(float m, float l) {
-  if (m == -INFINITY && l == 0.0f) return 0.0f;
-  return fabsf(m) <= 0x1p28f ? l : NAN;
-}
+// A weight is 2 to the power of its logit (times log2 e) less a reference m, which lies at most 8 under the largest.  The key that
+// set m has a weight of 2^d, d being what m lost when it was rounded: nothing that matters up to 2^28, where d is 16 at
+// most and the row's sum takes it out again; beyond, that weight could be anything, 0 and infinity among it.  So logits
+// under -2^28 weigh nothing, like masked ones (a split may hold no others), and a reference over 2^28 gives a row of NaN.
+constexpr float kFarLogit = 0x1p28f;
+__device__ __forceinline__ float reference(float m) { return m < -kFarLogit ? 0.0f : m; }
+// The sum that a row's outputs are divided by: 0 for a row of no weight, NaN for one that has no sum.
+__device__ __forceinline__ float row_sum(float m, float l) { return m <= kFarLogit ? l : NAN; }
 
 // ---------------------------------------------------------------------------------------------
 // Attention of many rows.  The layout is that of the kernel over bf16 pages (kernels.hip): a workgroup of NW waves
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q4_kernel(DevPl
       // well as values below 1.  The final normalization uses the same reference.
       const bool bump = mx > m_run + 8.0f;
       const float m_new = bump ? mx : m_run;
-      const float m_use = (m_new == -INFINITY) ? 0.0f : m_new;
+      const float m_use = reference(m_new);
       float rs = 0.0f;
       bf16x8 pb[2 * NKB];
 #pragma unroll
@@ -546,7 +547,7 @@ __global__ __launch_bounds__(256, 2) void attn_q4_few_kernel(DevPlan p, const __
     mx = halves_max(mx) * sl2;
     const bool bump = mx > m_run + 8.0f;         // as in the kernel above
     const float m_new = bump ? mx : m_run;
-    const float m_use = (m_new == -INFINITY) ? 0.0f : m_new;
+    const float m_use = reference(m_new);
     float rs = 0.0f;
     bf16x8 pb[2];
 #pragma unroll

@@ -91,10 +91,26 @@ def test_one_bad_number_of_a_key_with_a_finite_logit(name, splits):
     clean, g, seen = run(name, splits, spoil(-1.0))
     assert same(clean["out"][~seen], g["out"][~seen]) and same(clean["lse"][~seen], g["lse"][~seen])
     q, kv, dim, page, prefix, chunk = WAVES[name]
-    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=71, name=name)
-    k, v = (oracle.q4.pool_values(g[n].cpu().numpy(), dim, page) for n in ("k_pool", "v_pool"))
+    right(wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=71, name=name), g)
+
+
+def right(spec, g):
+    """Whether the outputs are the oracle's over the values that the cache holds."""
+    k, v = (oracle.q4.pool_values(g[n].cpu().numpy(), spec.head_dim_qk, spec.page_size) for n in ("k_pool", "v_pool"))
     with np.errstate(over="ignore", invalid="ignore"):
-        o, lse, size = oracle.q4.attention(wl.to_bits(g["q"].cpu()), k, v, spec.prefix_lens, spec.chunk_lens, spec.block_table, page,
-                                           spec.softmax_scale)
+        o, lse, size = oracle.q4.attention(wl.to_bits(g["q"].cpu()), k, v, spec.prefix_lens, spec.chunk_lens, spec.block_table,
+                                           spec.page_size, spec.softmax_scale)
     assert (np.abs(g["out"].float().cpu().numpy() - o) <= MERGED * size).all()
     assert (np.abs(g["lse"].cpu().numpy() - lse) <= LSE).all()
+
+
+@pytest.mark.parametrize("dim,page", [(128, 64), (64, 16)])
+@pytest.mark.parametrize("chunk", [1, 9, 40])
+@pytest.mark.parametrize("splits", [1, 9, 17])
+def test_a_key_far_below_zero_alone_in_its_split(dim, page, chunk, splits):
+    """The first new token begins a tile, and a split where a tile is one: its row sees no other key there."""
+    spec = wl.custom_wave(16, 2, dim, dim, page, [1024, 70], [chunk, 1], seed=76, name="alone")
+    t = make(spec, 77)
+    t["k_new"][0, :, 5] = float("nan")
+    t["q"][:chunk, :, 5] = -t["q"][:chunk, :, 5].abs() - 0.25
+    right(spec, on_gpu(spec, t, max_splits=splits))
