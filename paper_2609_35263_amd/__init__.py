@@ -1,9 +1,9 @@
-"""Chunked-prefill attention over a paged KV cache of bf16 or of 4-bit values, and chunked prefill of KDA
-(gated delta-rule) layers and of linear-attention layers with a decay for each head, with recurrent-state
-snapshots, on AMD MI355X (gfx950).
+"""Chunked-prefill attention over a paged KV cache of bf16, of 8-bit or of 4-bit values, rotary positions for the
+rows of all of them, and chunked prefill of KDA (gated delta-rule) layers and of linear-attention layers with
+a decay for each head, with recurrent-state snapshots, on AMD MI355X (gfx950).
 
 Thin Python binding of libwavepp_attn.so (C ABI declared in include/wavepp_attn.h, include/wavepp_q4.h,
-include/wavepp_kda.h and include/wavepp_lin.h).  Every step of
+include/wavepp_q8.h, include/wavepp_rope.h, include/wavepp_kda.h and include/wavepp_lin.h).  Every step of
 the computation runs in the library's HIP kernels; this module only marshals arguments: torch
 tensors are passed as device pointers, the stream is torch's current HIP stream.
 
@@ -20,6 +20,15 @@ Per wave over 4-bit pages, single tokens (decoding) included:
     plan_upload(p, ws)
     q4_append_kv(p, k_new, v_new, k_pool, v_pool, ws)        # pools from q4_new_pool
     q4_chunked_prefill(p, q, k_pool, v_pool, out, lse, ws)
+
+Per wave over 8-bit pages, with rotary positions and with scores beyond the causal ones where the layer has them:
+    rope = Rope(rot_dim=...)            # once per model
+    p = q8_plan(..., score_cap=..., slopes=..., key_begin=..., key_end=...)
+    ws = new_workspace(p)
+    plan_upload(p, ws)
+    rope_apply(rope, p, q, k_new, q, k_new, ws)              # in place; a plan of any cache will do
+    q8_append_kv(p, k_new, v_new, k_pool, v_pool, ws)        # pools from q8_new_pool
+    q8_chunked_prefill(p, q, k_pool, v_pool, out, lse, ws)
 
 Per wave of a KDA layer:
     kp = kda_plan(...)                  # host: validate chunk lengths and snapshot slots
@@ -57,7 +66,11 @@ LIN_SYMBOLS = [
     "wavepp_lin_plan", "wavepp_lin_workspace_bytes", "wavepp_lin_get_info", "wavepp_lin_upload",
     "wavepp_lin_chunked_prefill", "wavepp_lin_destroy",
 ]
-EXPORTED_SYMBOLS += Q4_SYMBOLS + LIN_SYMBOLS
+Q8_SYMBOLS = [
+    "wavepp_q8_page_bytes", "wavepp_q8_plan", "wavepp_q8_append_kv", "wavepp_q8_read_kv", "wavepp_q8_chunked_prefill",
+]
+ROPE_SYMBOLS = ["wavepp_rope_create", "wavepp_rope_frequencies", "wavepp_rope_apply", "wavepp_rope_destroy"]
+EXPORTED_SYMBOLS += Q4_SYMBOLS + LIN_SYMBOLS + Q8_SYMBOLS + ROPE_SYMBOLS
 MPU_SYMBOLS = [
     "wavepp_mpu_budget_ladder", "wavepp_mpu_create", "wavepp_mpu_admit", "wavepp_mpu_plan", "wavepp_mpu_commit",
     "wavepp_mpu_retire", "wavepp_mpu_get_state", "wavepp_mpu_destroy",
@@ -90,6 +103,17 @@ class _Shape(ctypes.Structure):
 class _Batch(ctypes.Structure):
     _fields_ = [("num_requests", ctypes.c_int32), ("prefix_lens", ctypes.c_void_p), ("chunk_lens", ctypes.c_void_p),
                 ("block_table", ctypes.c_void_p), ("bt_stride", ctypes.c_int32)]
+
+
+class _Scores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("key_begin", ctypes.c_void_p),
+                ("key_end", ctypes.c_void_p)]
+
+
+class _RopeSpec(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "rot_offset", "interleaved", "scaling")] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "original_length", "slow_turns", "fast_turns", "magnitude")] + \
+               [("frequencies", ctypes.c_void_p)]
 
 
 class _Info(ctypes.Structure):
@@ -178,6 +202,24 @@ def load_library(path: str = None) -> ctypes.CDLL:
         getattr(lib, name).restype = ctypes.c_int
     lib.wavepp_q4_chunked_prefill.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.wavepp_q4_chunked_prefill.restype = ctypes.c_int
+    lib.wavepp_q8_page_bytes.argtypes = [i32, i32]
+    lib.wavepp_q8_page_bytes.restype = sz
+    lib.wavepp_q8_plan.argtypes = [ctypes.POINTER(_Shape), ctypes.POINTER(_Batch), ctypes.POINTER(_Scores), i32, ctypes.POINTER(vp)]
+    lib.wavepp_q8_plan.restype = ctypes.c_int
+    for name in ("wavepp_q8_append_kv", "wavepp_q8_read_kv"):
+        getattr(lib, name).argtypes = [vp, vp, vp, vp, vp, vp, sz, vp]
+        getattr(lib, name).restype = ctypes.c_int
+    lib.wavepp_q8_chunked_prefill.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.wavepp_q8_chunked_prefill.restype = ctypes.c_int
+    stride = ctypes.c_int64
+    lib.wavepp_rope_create.argtypes = [ctypes.POINTER(_RopeSpec), ctypes.POINTER(vp)]
+    lib.wavepp_rope_create.restype = ctypes.c_int
+    lib.wavepp_rope_frequencies.argtypes = [vp, ctypes.POINTER(ctypes.c_double), i32]
+    lib.wavepp_rope_frequencies.restype = ctypes.c_int
+    lib.wavepp_rope_apply.argtypes = [vp, vp, vp, stride, vp, stride, vp, stride, vp, stride, vp, vp, sz, vp]
+    lib.wavepp_rope_apply.restype = ctypes.c_int
+    lib.wavepp_rope_destroy.argtypes = [vp]
+    lib.wavepp_rope_destroy.restype = None
     lib.wavepp_plan_destroy.argtypes = [vp]
     lib.wavepp_plan_destroy.restype = None
     lib.wavepp_status_string.argtypes = [ctypes.c_int]
@@ -289,7 +331,7 @@ class Plan:
 
 
 def _plan(entry, *, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
-          prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0) -> Plan:
+          prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0, more=()) -> Plan:
     lib = load_library()
     prefix = np.ascontiguousarray(prefix_lens, dtype=np.int32)
     chunk = np.ascontiguousarray(chunk_lens, dtype=np.int32)
@@ -302,7 +344,7 @@ def _plan(entry, *, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_siz
                    float(softmax_scale))
     batch = _Batch(prefix.shape[0], prefix.ctypes.data, chunk.ctypes.data, bt.ctypes.data, bt.shape[1])
     out = ctypes.c_void_p()
-    _check(getattr(lib, entry)(ctypes.byref(shape), ctypes.byref(batch), int(max_splits), ctypes.byref(out)))
+    _check(getattr(lib, entry)(ctypes.byref(shape), ctypes.byref(batch), *more, int(max_splits), ctypes.byref(out)))
     return Plan(out.value, dict(num_q_heads=num_q_heads, num_kv_heads=num_kv_heads, head_dim_qk=head_dim_qk,
                                 head_dim_v=head_dim_v, page_size=page_size, num_pages=num_pages,
                                 kv_shared=bool(kv_shared), softmax_scale=float(softmax_scale),
@@ -566,6 +608,197 @@ def q4_chunked_prefill(p: Plan, q, k_pool, v_pool, out, lse, workspace, stream=N
     args = _call_args(stream, *bufs)
     _check(load_library().wavepp_q4_chunked_prefill(p.handle, *args[:4], None if lse is None else args[5], args[4],
                                                     workspace.nbytes, args[-1]))
+
+
+# ------------------------------------------------------------------------------------------------
+# 8-bit paged cache
+# ------------------------------------------------------------------------------------------------
+
+def q8_page_bytes(head_dim, page_size) -> int:
+    """Bytes of one page of one KV head: one a value, and 16."""
+    n = int(load_library().wavepp_q8_page_bytes(int(head_dim), int(page_size)))
+    if not n:
+        raise ValueError(f"an 8-bit cache has head dims 64 and 128 and pages of 16 and 64 tokens, not {head_dim}, {page_size}")
+    return n
+
+
+def q8_new_pool(num_pages, num_kv_heads, head_dim, page_size, device=None):
+    """A pool of 8-bit pages, K's or V's, all values zero."""
+    import torch
+    return torch.zeros((num_pages, num_kv_heads, q8_page_bytes(head_dim, page_size)), dtype=torch.uint8,
+                       device=device or "cuda")
+
+
+def q8_plan(*, num_q_heads, num_kv_heads, head_dim_qk, head_dim_v, page_size, num_pages, softmax_scale,
+            prefix_lens, chunk_lens, block_table, kv_shared=False, max_splits=0, score_cap=0.0, slopes=None,
+            key_begin=None, key_end=None) -> Plan:
+    """plan() for a wave over 8-bit pages (plan_upload and new_workspace take it too), with the layer's scores: capped to
+    score_cap tanh(s / score_cap) where that is not 0, less slopes[head] times the distance of the key, and for each new
+    token only over the keys key_begin[t] <= j < key_end[t] of its request (None: from 0, up to its own position)."""
+    tokens = int(np.add.reduce(np.asarray(chunk_lens, dtype=np.int64)))
+    arrays = []
+    for name, a, dtype, n in (("slopes", slopes, np.float32, int(num_q_heads)), ("key_begin", key_begin, np.int32, tokens),
+                              ("key_end", key_end, np.int32, tokens)):
+        if a is not None:
+            given = np.asarray(a)
+            a = np.ascontiguousarray(given, dtype=dtype)
+            if a.shape != (n,):
+                raise ValueError(f"{name} has shape {a.shape}, the wave needs {(n,)}")
+            if dtype is np.int32 and not np.array_equal(a, given):
+                raise ValueError(f"{name} must hold whole numbers of 32 bits")
+        arrays.append(a)
+    scores = None
+    if score_cap or any(a is not None for a in arrays):
+        # (an empty array has no address of its own to pass)
+        scores = ctypes.byref(_Scores(float(score_cap), *(None if a is None or a.size == 0 else a.ctypes.data for a in arrays)))
+    p = _plan("wavepp_q8_plan", num_q_heads=num_q_heads, num_kv_heads=num_kv_heads, head_dim_qk=head_dim_qk,
+              head_dim_v=head_dim_v, page_size=page_size, num_pages=num_pages, softmax_scale=softmax_scale,
+              prefix_lens=prefix_lens, chunk_lens=chunk_lens, block_table=block_table, kv_shared=kv_shared,
+              max_splits=max_splits, more=(scores,))
+    p._buffers = {**_attn_shapes(p), "pool8": (int(num_pages), int(num_kv_heads), q8_page_bytes(head_dim_qk, page_size))}
+    return p
+
+
+def q8_plan_for(spec, max_splits=0, **scores) -> Plan:
+    """plan_for() for a wave over 8-bit pages."""
+    return q8_plan(num_q_heads=spec.num_q_heads, num_kv_heads=spec.num_kv_heads, head_dim_qk=spec.head_dim_qk,
+                   head_dim_v=spec.head_dim_v, page_size=spec.page_size, num_pages=spec.num_pages,
+                   softmax_scale=spec.softmax_scale, prefix_lens=spec.prefix_lens, chunk_lens=spec.chunk_lens,
+                   block_table=spec.block_table, kv_shared=spec.kv_shared, max_splits=max_splits, **scores)
+
+
+def _q8_shapes(p: Plan) -> dict:
+    sh = _attn_shapes(p)
+    if "pool8" not in sh:
+        raise ValueError("the plan is of another cache: make it with q8_plan")
+    return sh
+
+
+def q8_append_kv(p: Plan, k_new, v_new, k_pool, v_pool, workspace, stream=None):
+    """Round the wave's new K/V rows into their pages."""
+    bf, u8 = _torch_types()[:2]
+    sh = _q8_shapes(p)
+    k, v, kp, vp, ws, st = _call_args(stream, ("k_new", k_new, sh["k_new"], bf), ("v_new", v_new, sh["v_new"], bf),
+                                      ("k_pool", k_pool, sh["pool8"], u8), ("v_pool", v_pool, sh["pool8"], u8),
+                                      ("workspace", workspace, None, None))
+    _check(load_library().wavepp_q8_append_kv(p.handle, k, v, kp, vp, ws, workspace.nbytes, st))
+
+
+def q8_read_kv(p: Plan, k_pool, v_pool, k_out, v_out, workspace, stream=None):
+    """The bf16 rows of the wave's new tokens as the pages hold them."""
+    bf, u8 = _torch_types()[:2]
+    sh = _q8_shapes(p)
+    kp, vp, k, v, ws, st = _call_args(stream, ("k_pool", k_pool, sh["pool8"], u8), ("v_pool", v_pool, sh["pool8"], u8),
+                                      ("k_out", k_out, sh["k_new"], bf), ("v_out", v_out, sh["v_new"], bf),
+                                      ("workspace", workspace, None, None))
+    _check(load_library().wavepp_q8_read_kv(p.handle, kp, vp, k, v, ws, workspace.nbytes, st))
+
+
+def q8_chunked_prefill(p: Plan, q, k_pool, v_pool, out, lse, workspace, stream=None):
+    """Attention of the wave's queries over 8-bit pages, with the plan's scores (lse may be None)."""
+    bf, u8, f32 = _torch_types()
+    sh = _q8_shapes(p)
+    bufs = [("q", q, sh["q"], bf), ("k_pool", k_pool, sh["pool8"], u8), ("v_pool", v_pool, sh["pool8"], u8),
+            ("out", out, sh["out"], bf), ("workspace", workspace, None, None)]
+    if lse is not None:
+        bufs.append(("lse", lse, sh["lse"], f32))
+    args = _call_args(stream, *bufs)
+    _check(load_library().wavepp_q8_chunked_prefill(p.handle, *args[:4], None if lse is None else args[5], args[4],
+                                                    workspace.nbytes, args[-1]))
+
+
+# ------------------------------------------------------------------------------------------------
+# Rotary positions
+# ------------------------------------------------------------------------------------------------
+
+_ROPE_SCALING = {"none": 0, "linear": 1, "turns": 2, "index": 3}
+
+
+class Rope:
+    """Which values of a head are turned, and how fast (host object owned by the library).
+
+    Pair i of rot_dim / 2, the values rot_offset + i and rot_offset + rot_dim / 2 + i, or with interleaved rot_offset + 2 i
+    and the next, turns by frequencies[i] radians a token: base ** (-2 i / rot_dim), with scaling "linear", "turns" or "index"
+    for contexts longer than original_length (see include/wavepp_rope.h), or the given frequencies."""
+
+    def __init__(self, *, rot_dim, rot_offset=0, interleaved=False, base=10000.0, scaling="none", factor=1.0,
+                 original_length=0.0, slow_turns=0.0, fast_turns=0.0, magnitude=1.0, frequencies=None):
+        self._h = ctypes.c_void_p(None)
+        if scaling not in _ROPE_SCALING:
+            raise ValueError(f"scaling must be one of {sorted(_ROPE_SCALING)}, not {scaling!r}")
+        table = None
+        if frequencies is not None:
+            table = np.ascontiguousarray(frequencies, dtype=np.float64)
+            if table.shape != (int(rot_dim) // 2,):
+                raise ValueError(f"frequencies has shape {table.shape}, rot_dim needs {(int(rot_dim) // 2,)}")
+        spec = _RopeSpec(int(rot_dim), int(rot_offset), int(bool(interleaved)), _ROPE_SCALING[scaling], float(base),
+                         float(factor), float(original_length), float(slow_turns), float(fast_turns), float(magnitude),
+                         None if table is None or table.size == 0 else table.ctypes.data)
+        out = ctypes.c_void_p()
+        _check(load_library().wavepp_rope_create(ctypes.byref(spec), ctypes.byref(out)))
+        self._h = out
+        self.rot_dim = int(rot_dim)
+
+    @property
+    def handle(self):
+        if not self._h:
+            raise ValueError("rope was destroyed")
+        return self._h
+
+    def frequencies(self) -> np.ndarray:
+        buf = np.zeros(self.rot_dim // 2, dtype=np.float64)
+        n = load_library().wavepp_rope_frequencies(self.handle, buf.ctypes.data_as(ctypes.POINTER(ctypes.c_double)), len(buf))
+        if n < 0:
+            _check(n)
+        return buf[:n]
+
+    def destroy(self):
+        if self._h:
+            load_library().wavepp_rope_destroy(self._h)
+            self._h = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _row_args(here, name, t, shape, dtype):
+    """(address, elements from token to token) of rows [T, heads, dim] whose tokens may lie apart."""
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}, the current device is {here}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the plan needs {shape}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    s = t.stride()
+    if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name} must be contiguous within a token, its strides are {s}")
+    return t.data_ptr(), s[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def rope_apply(rope: Rope, p: Plan, q, k, q_out, k_out, workspace, positions=None, stream=None):
+    """Turn the query and key rows of the plan's new tokens by their positions (or by positions, int32 [T] on the device).
+    q_out is q, or a tensor apart from all others; so with k, and either pair may be None.  Tokens may lie apart, as in slices of
+    one packed projection."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    sh = _attn_shapes(p)
+    for name, t, t_out in (("q", q, q_out), ("k", k, k_out)):
+        if (t is None) != (t_out is None):
+            raise ValueError(f"{name} and {name}_out come together")
+    args = []
+    for name, t, t_out, shape in (("q", q, q_out, sh["q"]), ("k", k, k_out, sh["k_new"])):
+        args.append((None, 0, None, 0) if t is None else (*_row_args(here, name, t, shape, torch.bfloat16),
+                                                         *_row_args(here, name + "_out", t_out, shape, torch.bfloat16)))
+    bufs = [("workspace", workspace, None, None)]
+    if positions is not None:
+        bufs.append(("positions", positions, (sh["q"][0],), torch.int32))
+    ws, *at, st = _call_args(stream, *bufs)
+    (q_at, q_s, qo_at, qo_s), (k_at, k_s, ko_at, ko_s) = args
+    _check(load_library().wavepp_rope_apply(rope.handle, p.handle, q_at, q_s, k_at, k_s, qo_at, qo_s, ko_at, ko_s,
+                                            at[0] if at else None, ws, workspace.nbytes, st))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -9,6 +9,7 @@
 #include "internal.h"
 #include "plan.h"
 #include "q4.h"
+#include "q8.h"
 
 #include <hip/hip_runtime.h>
 
@@ -647,10 +648,13 @@ int check_workspace(const wavepp_plan* plan, void* ws, size_t ws_bytes) {
   return WAVEPP_OK;
 }
 
-int require_cache(const wavepp_plan* plan, bool q4) {
-  if (plan->q4 == q4) return WAVEPP_OK;
-  return plan->q4 ? set_error(WAVEPP_EINVAL, "the plan is of a 4-bit cache: use the wavepp_q4 entry points")
-                  : set_error(WAVEPP_EINVAL, "the plan is of a bf16 cache: make it with wavepp_q4_plan");
+int require_cache(const wavepp_plan* plan, Cache cache) {
+  if (plan->cache == cache) return WAVEPP_OK;
+  if (plan->cache == Cache::q4)
+    return set_error(WAVEPP_EINVAL, "the plan is of a 4-bit cache: use the wavepp_q4 entry points");
+  if (plan->cache == Cache::q8)
+    return set_error(WAVEPP_EINVAL, "the plan is of an 8-bit cache: use the wavepp_q8 entry points");
+  return set_error(WAVEPP_EINVAL, "the plan is of a bf16 cache: make it with wavepp_%s_plan", cache == Cache::q4 ? "q4" : "q8");
 }
 
 DevPlan make_dev(const wavepp_plan* plan, void* ws) {
@@ -681,8 +685,8 @@ DevPlan make_dev(const wavepp_plan* plan, void* ws) {
   return d;
 }
 
-int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, bool q4,
-              wavepp_plan** out) {
+int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, Cache cache,
+              const PlanScores* scores, wavepp_plan** out) {
   clear_error();
   if (!shape || !batch || !out) return set_error(WAVEPP_EINVAL, "null argument");
   *out = nullptr;
@@ -696,9 +700,10 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     return set_error(WAVEPP_EINVAL, "num_q_heads (%d) is not a multiple of num_kv_heads (%d)", s.num_q_heads,
                 s.num_kv_heads);
   if (s.kv_shared != 0 && s.kv_shared != 1) return set_error(WAVEPP_EINVAL, "kv_shared must be 0 or 1");
-  if (!supported_shape(s) || (q4 && s.kv_shared))
+  const bool bits = cache != Cache::bf16;
+  if (!supported_shape(s) || (bits && s.kv_shared))
     return set_error(WAVEPP_EUNSUPPORTED, "unsupported%s (head_dim_qk=%d, head_dim_v=%d, page_size=%d, kv_shared=%d, "
-                "num_kv_heads=%d)", q4 ? " for a 4-bit cache" : "", s.head_dim_qk, s.head_dim_v, s.page_size, s.kv_shared,
+                "num_kv_heads=%d)", cache == Cache::q4 ? " for a 4-bit cache" : bits ? " for an 8-bit cache" : "", s.head_dim_qk, s.head_dim_v, s.page_size, s.kv_shared,
                 s.num_kv_heads);
   if (max_splits < 0) return set_error(WAVEPP_EINVAL, "max_splits must be >= 0");
   const int32_t R = batch->num_requests;
@@ -740,11 +745,30 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
         return set_error(WAVEPP_EALIAS, "request %d block %lld: page %d receives appended tokens but is referenced %d "
                     "times in the wave", r, (long long)b, row[b], refcount[row[b]]);
   }
+  if (scores) {
+    if (!(scores->cap >= 0.0f) || !std::isfinite(scores->cap))
+      return set_error(WAVEPP_EINVAL, "the scores' cap must be finite and not negative");
+    if (scores->cap > 0.0f && !(scores->cap >= 1e-3f && scores->cap <= 1e6f))
+      return set_error(WAVEPP_EINVAL, "the scores' cap must lie in [1e-3, 1e6], or be 0 for none");
+    if (scores->slopes)
+      for (int32_t h = 0; h < s.num_q_heads; ++h)
+        if (!(std::fabs(scores->slopes[h]) <= 1024.0f))
+          return set_error(WAVEPP_EINVAL, "head %d: a slope must be a number within [-1024, 1024]", h);
+    int64_t t = 0;
+    for (int32_t r = 0; r < R; ++r) {
+      const int64_t n = int64_t(batch->prefix_lens[r]) + batch->chunk_lens[r];
+      for (int32_t i = 0; i < batch->chunk_lens[r]; ++i, ++t)
+        for (const int32_t* at : {scores->key_begin, scores->key_end})
+          if (at && (at[t] < 0 || at[t] > n))
+            return set_error(WAVEPP_EINVAL, "request %d token %d: its keys begin or end at %d, outside [0, %lld]", r, i, at[t],
+                             (long long)n);
+    }
+  }
 
   std::unique_ptr<wavepp_plan> plan(new (std::nothrow) wavepp_plan());
   if (!plan) return set_error(WAVEPP_EINVAL, "out of host memory");
   plan->shape = s;
-  plan->q4 = q4;
+  plan->cache = cache;
   plan->num_requests = R;
   plan->bt_stride = stride;
   plan->total_tokens = total;
@@ -755,12 +779,12 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   // chunks: the wave is bound by streaming the prefix K/V), half of those waves would idle: the
   // plan then uses 128-row items, run by the 4-wave form of the kernel, two workgroups per CU.
   // WAVEPP_GQA_WAVES=4 or 8 forces one form.
-  // Over 4-bit pages, requests of up to 32 rows a KV head -- a token or a few -- run with one wave's rows and the
+  // Over 4-bit and 8-bit pages, requests of up to 32 rows a KV head -- a token or a few -- run with one wave's rows and the
   // keys of a tile shared out over the four waves of a workgroup, in a launch of their own beside longer chunks.
   const char* gw = getenv("WAVEPP_GQA_WAVES");
   const int gw_n = gw ? atoi(gw) : 0;
   auto rows_of = [&](int32_t r) { return int64_t(batch->chunk_lens[r]) * G; };
-  auto is_few = [&](int32_t r) { return q4 && gw_n == 0 && rows_of(r) <= kQ4FewRows; };
+  auto is_few = [&](int32_t r) { return bits && gw_n == 0 && rows_of(r) <= kQ4FewRows; };
   int64_t max_rows = 0;
   bool any_few = false;
   for (int32_t r = 0; r < R; ++r) {
@@ -784,6 +808,18 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       if (is_few(r)) many_lens[r] = 0;
     many.chunk_lens = many_lens.data();
   }
+  // the keys that a new token sees, where the scores say it
+  const bool ranged = scores && (scores->key_begin || scores->key_end);
+  std::vector<TokenRange> ranges;
+  if (ranged) {
+    ranges.reserve(size_t(total));
+    for (int32_t r = 0; r < R; ++r)
+      for (int32_t i = 0; i < batch->chunk_lens[r]; ++i) {
+        const size_t t = ranges.size();
+        ranges.push_back({scores->key_begin ? scores->key_begin[t] : 0,
+                          scores->key_end ? scores->key_end[t] : batch->prefix_lens[r] + i + 1});
+      }
+  }
   int64_t part_rows = 0;
   int max_used = 1;
 
@@ -799,10 +835,21 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       plan->kv_tile = KT;
     }
     std::vector<WorkItem> base;
+    std::vector<TokenRange> seen;
     for (int32_t r = 0; r < R; ++r) {
       if (is_few(r) != few_rows) continue;
       const int32_t p = batch->prefix_lens[r];
       const int64_t rows_total = rows_of(r);
+      if (few_rows) plan->few_rows = std::max(plan->few_rows, int32_t(rows_total));
+      seen.clear();
+      for (int64_t r0 = 0; ranged && r0 < rows_total; r0 += M) {
+        TokenRange u{INT32_MAX, 0};                 // all keys of the tile's tokens, from a tile's first
+        for (int64_t t = r0 / G; t <= (std::min<int64_t>(r0 + M, rows_total) - 1) / G; ++t) {
+          const TokenRange& x = ranges[size_t(reqs[r].cu + t)];
+          if (x.begin < x.end) u = {std::min(u.begin, x.begin), std::max(u.end, x.end)};
+        }
+        seen.push_back(u.begin < u.end ? TokenRange{u.begin / KT * KT, u.end} : TokenRange{0, 0});
+      }
       for (int32_t g = 0; g < s.num_kv_heads; ++g)
         for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
           WorkItem w{};
@@ -811,8 +858,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
           w.row0 = int32_t(r0);
           w.rows = int32_t(std::min<int64_t>(M, rows_total - r0));
           const int64_t last_tok = (r0 + w.rows - 1) / G;
-          w.kv_begin = 0;
-          w.kv_end = int32_t(p + last_tok + 1);
+          w.kv_begin = ranged ? seen[size_t(r0 / M)].begin : 0;
+          w.kv_end = ranged ? seen[size_t(r0 / M)].end : int32_t(p + last_tok + 1);
           w.part = -1;
           w.split = 0;
           base.push_back(w);
@@ -831,7 +878,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     const int64_t fill_target = 512;
     const int64_t min_split_tiles = (mla ? 512 : few_rows ? 256 : 1024) / KT;
     std::vector<int64_t> ntiles(base.size());
-    for (size_t i = 0; i < base.size(); ++i) ntiles[i] = ceil_div(base[i].kv_end, KT);
+    for (size_t i = 0; i < base.size(); ++i)
+      ntiles[i] = std::max<int64_t>(1, ceil_div(base[i].kv_end - base[i].kv_begin, KT));
     SplitPlan split{ntiles, int64_t(base.size())};
     if (max_splits >= 1) {
       for (size_t i = 0; i < base.size(); ++i) split.tps[i] = ceil_div(ntiles[i], std::min<int64_t>(max_splits, ntiles[i]));
@@ -872,7 +920,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       // faster wherever it says so on the timed waves (one request of 8K-40K cached tokens, 64/8 heads, 304 rows
       // per KV head: 67.5 us as 352 items, 54.6 as 256), while 256 items always would lose 15 % on average.
       int64_t target = fill_target;
-      if (!mla && !small_rows && int64_t(base.size()) < kNumCu && longest >= 2 * min_split_tiles &&
+      // (The model knows causal waves alone.)
+      if (!mla && !small_rows && !ranged && int64_t(base.size()) < kNumCu && longest >= 2 * min_split_tiles &&
           grouped_cost(s, many, kNumCu, 1024) < 0.95 * grouped_cost(s, many, fill_target, 1024))
         target = kNumCu;
       split = even(target);
@@ -940,8 +989,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       plan->merges.push_back(m);
       for (int64_t si = 0; si < S; ++si) {
         WorkItem x = w;
-        x.kv_begin = int32_t(si * tps * KT);
-        x.kv_end = int32_t(std::min<int64_t>(w.kv_end, (si + 1) * tps * KT));
+        x.kv_begin = int32_t(w.kv_begin + si * tps * KT);
+        x.kv_end = int32_t(std::min<int64_t>(w.kv_end, w.kv_begin + (si + 1) * tps * KT));
         x.part = int32_t(part_rows + si * w.rows);
         x.split = int32_t(si);
         items.push_back(x);
@@ -978,6 +1027,30 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   off = align_up(off + sizeof(WorkItem) * plan->items.size(), 16);
   plan->off_merges = off;
   off = align_up(off + sizeof(MergeItem) * plan->merges.size(), 16);
+  // 8-bit pages: one record for each block of 16 slots that receives tokens, request by request
+  std::vector<Q8Block> blocks;
+  if (cache == Cache::q8) {
+    for (int32_t r = 0; r < R; ++r) {
+      const int64_t p = batch->prefix_lens[r], n = p + batch->chunk_lens[r];
+      if (p == n) continue;
+      for (int64_t at = p / kQ8Block * kQ8Block; at < n; at += kQ8Block)
+        blocks.push_back({batch->block_table[int64_t(r) * stride + at / B], int32_t(at % B),
+                          int32_t(reqs[r].cu + std::max(at, p) - p),
+                          int32_t(std::max<int64_t>(p - at, 0) | (std::min<int64_t>(n - at, kQ8Block) << 8))});
+    }
+    plan->num_blocks = int32_t(blocks.size());
+    plan->off_blocks = off;
+    off = align_up(off + sizeof(Q8Block) * blocks.size(), 16);
+    if (ranged) {
+      plan->off_ranges = off;
+      off = align_up(off + sizeof(TokenRange) * ranges.size(), 16);
+    }
+    if (scores && scores->slopes) {
+      plan->off_slopes = off;
+      off = align_up(off + sizeof(float) * size_t(s.num_q_heads), 16);
+    }
+    if (scores) plan->cap = scores->cap;
+  }
   plan->blob.assign(off, 0);
   MetaHeader h{};
   h.magic = kMagic;
@@ -995,6 +1068,11 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     memcpy(plan->blob.data() + plan->off_items, plan->items.data(), sizeof(WorkItem) * plan->items.size());
   if (!plan->merges.empty())
     memcpy(plan->blob.data() + plan->off_merges, plan->merges.data(), sizeof(MergeItem) * plan->merges.size());
+  if (!blocks.empty()) memcpy(plan->blob.data() + plan->off_blocks, blocks.data(), sizeof(Q8Block) * blocks.size());
+  if (plan->off_ranges && total)
+    memcpy(plan->blob.data() + plan->off_ranges, ranges.data(), sizeof(TokenRange) * ranges.size());
+  if (plan->off_slopes)
+    memcpy(plan->blob.data() + plan->off_slopes, scores->slopes, sizeof(float) * size_t(s.num_q_heads));
   plan->meta_bytes = align_up(off, 256);
   plan->off_opart = plan->meta_bytes;
   plan->off_lpart = align_up(plan->off_opart + sizeof(float) * size_t(part_rows) * size_t(s.head_dim_v), 256);
@@ -1031,7 +1109,7 @@ const char* wavepp_last_error(void) { return last_error_text(); }
 
 int wavepp_attn_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits,
                      wavepp_plan** out) {
-  return guarded([&] { return plan_wave(shape, batch, max_splits, false, out); });
+  return guarded([&] { return plan_wave(shape, batch, max_splits, Cache::bf16, nullptr, out); });
 }
 
 size_t wavepp_plan_workspace_bytes(const wavepp_plan* plan) { return plan ? plan->workspace_bytes : 0; }
@@ -1074,7 +1152,7 @@ int wavepp_attn_append_kv(const wavepp_plan* plan, const void* k_new, const void
                           void* workspace, size_t ws_bytes, hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  int st = require_cache(plan, false);
+  int st = require_cache(plan, Cache::bf16);
   if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st) return st;
   const bool shared = plan->shape.kv_shared != 0;
@@ -1096,7 +1174,7 @@ int wavepp_attn_chunked_prefill(const wavepp_plan* plan, const void* q, const vo
                                 void* out, float* lse, void* workspace, size_t ws_bytes, hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  int st = require_cache(plan, false);
+  int st = require_cache(plan, Cache::bf16);
   if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st) return st;
   const bool shared = plan->shape.kv_shared != 0;
@@ -1124,7 +1202,7 @@ int wavepp_attn_chunked_prefill_noalloc(const wavepp_plan* plan, const void* q, 
                                         hipStream_t stream) {
   clear_error();
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  if (int st = require_cache(plan, false)) return st;
+  if (int st = require_cache(plan, Cache::bf16)) return st;
   if (plan->workspace_bytes > kNoAllocScratchBytes)
     return set_error(WAVEPP_ENOSPACE, "plan needs %zu bytes of scratch, the static scratch holds %zu: plan the wave "
                      "with fewer key-range splits (max_splits) or call wavepp_attn_chunked_prefill with a workspace",

@@ -861,7 +861,7 @@ template <int DV>
 __device__ __forceinline__ void merge_store(const DevPlan& p, const MergeItem& mi, int cu, int lrow, int c4, f32x4 acc,
                                             float wsum, float mx, __bf16* out, float* lse_out) {
   const int Hq = p.num_q_heads, G = Hq / p.num_kv_heads;
-  const float inv = 1.0f / wsum;
+  const float inv = wsum == 0.0f ? 0.0f : 1.0f / wsum;      // no split saw a key: zeros, as in a row that is not split
   const int row = mi.row0 + lrow;
   const int tok = row / G;
   const int head = mi.kv_head * G + (row - tok * G);

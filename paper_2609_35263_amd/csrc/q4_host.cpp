@@ -15,7 +15,7 @@ int check_call(const wavepp_plan* plan, void* workspace, size_t ws_bytes, bool* 
   clear_error();
   *run = false;
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
-  int st = require_cache(plan, true);
+  int st = require_cache(plan, Cache::q4);
   if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st || plan->total_tokens == 0) return st;
   *run = true;
@@ -39,7 +39,7 @@ size_t wavepp_q4_page_bytes(int32_t head_dim, int32_t page_size) {
 }
 
 int wavepp_q4_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t max_splits, wavepp_plan** out) {
-  return guarded([&] { return plan_wave(shape, batch, max_splits, true, out); });
+  return guarded([&] { return plan_wave(shape, batch, max_splits, Cache::q4, nullptr, out); });
 }
 
 int wavepp_q4_append_kv(const wavepp_plan* plan, const void* k_new, const void* v_new, void* k_pool, void* v_pool,

@@ -1,0 +1,42 @@
+// Layout shared by the host code (host.cpp, q8_host.cpp) and the kernels (q8.hip) of the 8-bit paged cache.  Not part of the
+// public ABI.
+#pragma once
+
+#include "internal.h"
+
+namespace wavepp {
+
+constexpr int kQ8Block = 16;               // tokens of one head that share a scale
+constexpr int kQ8ScaleBytes = 16;          // bytes of a page's scales: page_size / 16 of them, then padding
+
+// Keys that a new token sees: [begin, end), none where begin >= end.
+struct TokenRange {
+  int32_t begin, end;
+};
+
+// A block of 16 slots that receives tokens of the wave.
+struct alignas(16) Q8Block {
+  int32_t page;      // page of the pool
+  int32_t slot;      // the block's first slot in it
+  int32_t token;     // packed token of the first new slot
+  int32_t span;      // new slots of the block: from the low byte to before the next byte
+};
+
+// What the 8-bit cache's launches need beyond a DevPlan.
+struct Q8Dev {
+  const Q8Block* blocks;
+  int32_t num_blocks;
+  int32_t few_rows;            // most rows of an item that runs with few rows
+  const TokenRange* ranges;    // of every new token; NULL: causal
+  const float* slopes;         // of every query head; NULL: none
+  float cap;                   // 0: none
+};
+
+hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new, const void* v_new, void* k_pool,
+                            void* v_pool, hipStream_t stream);
+hipError_t launch_q8_read(const DevPlan& p, const Q8Dev& x, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
+                          hipStream_t stream);
+hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few, const void* q, const void* k_pool,
+                               const void* v_pool, void* out, float* lse, hipStream_t stream);
+
+}  // namespace wavepp

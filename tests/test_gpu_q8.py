@@ -1,0 +1,500 @@
+"""The 8-bit paged cache on the GPU against its fp64 oracle, through the C ABI.
+
+Tolerances, fixed before the first run.  Append and read: exact, bytes and bits.
+
+Attention.  The operands are the cached values exactly.  With R = softmax_scale sum |q k| of a row's worst visible key, d the
+head dim, n the visible keys, S the row's largest |score|, c the cap and F the largest slope times distance, a score is off
+by at most
+    E = (d + 4) 2^-24 R + 2^-20 S + (2^-21 c where capped) + 2^-22 F
+(a sum of d products in fp32; the scale, log2 e and the reference subtracted, each a rounding of the score's size; the tanh as
+its header says; the distance's product and its subtraction), so a weight by E of itself, and the weights' fp32 sum by n 2^-24
+of itself at worst.  The LSE is off by no more than E + n 2^-24 + 2^-20.  What is rounded to bf16 is every probability (half a
+step, 2^-8 of itself) and the output (2^-8 of itself), so with size = sum p |v| an output is off by at most
+    2^-8 size + 2^-8 |o| + (2 (E + n 2^-24) + 2^-20) size.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_35263_amd as wp
+import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+
+def make(spec, seed, garbage=True, spread=0.5):
+    """q, k_new, v_new of tokens of unlike sizes, and pools whose cached slots hold rounded rows; the other slots hold any
+    bytes, codes that are not numbers among them, and so do the scales of blocks without a cached token and the padding."""
+    rng, any_bytes = np.random.default_rng(seed), np.random.default_rng(seed + 1000)
+    t = wl.make_tensors(spec, seed, poison=False)
+    P, H, B, d = spec.num_pages, spec.num_kv_heads, spec.page_size, spec.head_dim_qk
+    t = {n: t[n] for n in ("q", "k_new", "v_new")}
+    for n in ("k_new", "v_new"):
+        size = np.exp(spread * rng.standard_normal((spec.total_tokens, H, 1))).astype(np.float32)
+        t[n] = (t[n].float() * torch.from_numpy(size)).to(torch.bfloat16)
+    cnt = wl.prefix_slot_counts(spec)
+    used = np.arange(B)[None, :] < cnt[:, None]
+    for name in ("k_pool", "v_pool"):
+        x = rng.standard_normal((P, H, B, d)) * np.exp(spread * rng.standard_normal((P, H, B, 1)))
+        pool = oracle.q8.quantise_pool(np.where(used[:, None, :, None], x, 0.0))
+        if garbage:
+            codes, e, padding = (np.array(a) for a in oracle.q8.split_pool(pool, d, B))
+            codes = np.where(~used[:, None, :, None], any_bytes.integers(0, 256, codes.shape), codes)
+            empty = ~used.reshape(P, B // 16, 16).any(-1)
+            e = np.where(empty[:, None, :], any_bytes.integers(0, 256, e.shape), e)
+            pool = oracle.q8.join_pool(codes.astype(np.uint8), e, any_bytes.integers(0, 256, padding.shape))
+        t[name] = torch.from_numpy(pool)
+    return t
+
+
+def same(a, b):
+    """Whether two tensors hold the same bits."""
+    return bool(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)))
+
+
+def on_gpu(spec, t, max_splits=0, append=True, plan=None, **scores):
+    d = {n: x.cuda() for n, x in t.items()}
+    p = plan or wp.q8_plan_for(spec, max_splits=max_splits, **scores)
+    ws = wp.new_workspace(p)
+    out = torch.full((spec.total_tokens, spec.num_q_heads, spec.head_dim_v), float("nan"), dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((spec.total_tokens, spec.num_q_heads), float("nan"), device="cuda")
+    wp.plan_upload(p, ws)
+    if append:
+        wp.q8_append_kv(p, d["k_new"], d["v_new"], d["k_pool"], d["v_pool"], ws)
+    wp.q8_chunked_prefill(p, d["q"], d["k_pool"], d["v_pool"], out, lse, ws)
+    torch.cuda.synchronize()
+    return {**d, "out": out, "lse": lse, "plan": p, "ws": ws}
+
+
+def appended(spec, t):
+    d, B = spec.head_dim_qk, spec.page_size
+    return [oracle.q8.append(t[f"{n}_pool"].numpy(), wl.to_bits(t[f"{n}_new"]), spec.prefix_lens, spec.chunk_lens,
+                             spec.block_table, d, B) for n in "kv"]
+
+
+def score_errors(spec, q_bits, k, lse, cap=0.0, slopes=None, key_begin=None, key_end=None):
+    """(E, n) of the module's text for every row [T, Hq]; S is bounded by R and F, or by the cap and F."""
+    q = np.abs(oracle.bf16_bits_to_f64(q_bits))
+    k = np.abs(np.nan_to_num(k, nan=0.0))
+    T, Hq, d = q.shape
+    G = Hq // spec.num_kv_heads
+    E, N = np.zeros((T, Hq)), np.ones((T, Hq))
+    t = 0
+    for r in range(spec.num_requests):
+        p, c = int(spec.prefix_lens[r]), int(spec.chunk_lens[r])
+        pos = np.arange(p + c)
+        pages = np.asarray(spec.block_table[r], dtype=np.int64)[pos // spec.page_size]
+        for i in range(c):
+            a = 0 if key_begin is None else int(key_begin[t + i])
+            b = p + i + 1 if key_end is None else int(key_end[t + i])
+            if a >= b:
+                continue
+            far = np.abs(p + i - pos[a:b]).max()
+            for h in range(Hq):
+                K = k[pages[a:b], h // G, pos[a:b] % spec.page_size]
+                R = spec.softmax_scale * (K @ q[t + i, h]).max()
+                F = abs(float(slopes[h])) * far if slopes is not None else 0.0
+                S = (min(R, cap) if cap else R) + F
+                E[t + i, h] = (d + 4) * 2.0 ** -24 * R + 2.0 ** -20 * S + (2.0 ** -21 * cap if cap else 0.0) + 2.0 ** -22 * F
+                N[t + i, h] = b - a
+        t += c
+    return E, N
+
+
+def check(spec, t, g, what="", pools=None, **scores):
+    d, B = spec.head_dim_qk, spec.page_size
+    k, v = pools or appended(spec, t)
+    if pools is None:
+        assert np.array_equal(g["k_pool"].cpu().numpy(), k) and np.array_equal(g["v_pool"].cpu().numpy(), v), "pool bytes"
+    kv, vv = oracle.q8.pool_values(k, d, B), oracle.q8.pool_values(v, d, B)
+    bits = wl.to_bits(t["q"])
+    with np.errstate(over="ignore", invalid="ignore"):
+        o, lse, size = oracle.q8.attention(bits, kv, vv, spec.prefix_lens, spec.chunk_lens, spec.block_table, B,
+                                           spec.softmax_scale, **scores)
+        E, n = score_errors(spec, bits, kv, lse, **scores)
+    got, got_lse = g["out"].float().cpu().numpy().astype(np.float64), g["lse"].cpu().numpy().astype(np.float64)
+    bound = 2.0 ** -8 * (size + np.abs(o)) + (2 * (E + n * 2.0 ** -24) + 2.0 ** -20)[..., None] * size
+    err = np.abs(got - o)
+    blind = np.isneginf(lse)
+    assert np.isneginf(got_lse[blind]).all() and (got[blind] == 0).all(), "rows that see nothing"
+    lerr = np.abs(np.where(blind, 0.0, got_lse) - np.where(blind, 0.0, lse))
+    print(f"[q8] {spec.name} {what}: out {(err / np.maximum(bound, 1e-300)).max():.2f} of its bound, lse "
+          f"{(lerr / (E + n * 2.0 ** -24 + 2.0 ** -20)).max():.2f} of its", flush=True)
+    assert (err <= bound).all() and (lerr <= E + n * 2.0 ** -24 + 2.0 ** -20).all()
+
+
+def test_rounding_next_to_every_scale():
+    """Blocks whose largest magnitude is 1, 1.75, the next number and the last one under 2, times every power of two, filled with
+    bf16 numbers of at most that size from all over; and blocks of infinities and NaN.  Bytes, and the rows read back."""
+    rng = np.random.default_rng(1)
+    every = np.arange(0x8000, dtype=np.uint32)
+    blocks = []
+    for E in range(255):
+        for m in (0x00, 0x60, 0x61, 0x7F):
+            top = (E << 7) | m
+            # half from the top 2^20 of range, where codes are not zero, half from all below
+            near = rng.integers(max(0, top - (20 << 7)), top + 1, 512)
+            b = np.concatenate(([top], near, every[rng.integers(0, top + 1, 511)]))
+            blocks.append(b | (rng.integers(0, 2, 1024) << 15))
+    for odd in (0x7F80, 0xFF80, 0x7FC1, 0xFFFF):
+        b = rng.integers(0, 1 << 16, 1024)
+        b[:10] = odd
+        blocks.append(b)
+    rows = np.stack(blocks).astype(np.uint16).reshape(-1, 4, 16, 64).transpose(0, 2, 1, 3).reshape(-1, 4, 64)
+    T = rows.shape[0]
+    spec = wl.custom_wave(4, 4, 64, 64, 64, [0], [T], seed=1, name="rounding")
+    p = wp.q8_plan_for(spec)
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    new = torch.from_numpy(np.ascontiguousarray(rows).view(np.int16)).view(torch.bfloat16).cuda()
+    flipped = new.flip(1).contiguous()
+    pools = [wp.q8_new_pool(spec.num_pages, 4, 64, 64) for _ in range(2)]
+    back = [torch.empty_like(new) for _ in range(2)]
+    wp.q8_append_kv(p, new, flipped, *pools, ws)
+    wp.q8_read_kv(p, *pools, *back, ws)
+    torch.cuda.synchronize()
+    for pool, bits, got in zip(pools, (rows, rows[:, ::-1]), back):
+        want = oracle.q8.append(np.zeros(pool.shape, np.uint8), bits, [0], [T], spec.block_table, 64, 64)
+        assert np.array_equal(pool.cpu().numpy(), want)
+        pos = np.arange(T)
+        held = oracle.q8.pool_values(want, 64, 64)[spec.block_table[0][pos // 64], :, pos % 64]
+        assert np.array_equal(got.double().cpu().numpy(), held)
+
+
+def test_every_code_with_every_scale():
+    """Reading: all 256 codes with all exponents that an append writes, and codes that are not numbers."""
+    spec = wl.custom_wave(2, 2, 128, 128, 64, [0], [64 * 64], seed=2, name="codes", pool_slack=0.0)
+    P = spec.num_pages
+    rng = np.random.default_rng(3)
+    codes = np.stack([rng.permutation(np.tile(np.arange(256), 2 * 64 * 128 // 256)) for _ in range(P)])
+    codes = codes.reshape(P, 2, 64, 128).astype(np.uint8)
+    e = np.resize(np.arange(8, 247), P * 2 * 4).reshape(P, 2, 4).astype(np.uint8)
+    pool = torch.from_numpy(oracle.q8.join_pool(codes, e)).cuda()
+    p = wp.q8_plan_for(spec)
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    k = torch.empty(64 * 64, 2, 128, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    wp.q8_read_kv(p, pool, pool.flip(0).contiguous(), k, v, ws)
+    torch.cuda.synchronize()
+    held = oracle.q8.values(codes, np.repeat(e, 16, axis=-1)[..., None])
+    pos = np.arange(64 * 64)
+    pages = spec.block_table[0][pos // 64]
+    assert np.array_equal(k.double().cpu().numpy(), held[pages, :, pos % 64], equal_nan=True)
+    assert np.array_equal(v.double().cpu().numpy(), held[::-1][pages, :, pos % 64], equal_nan=True)
+
+
+@pytest.mark.parametrize("dim,page", [(128, 64), (64, 16), (64, 64), (128, 16)])
+def test_appends_in_pieces_grow_the_scales(dim, page):
+    """A wave after a wave into the same requests, with tokens of ever larger and smaller sizes: bytes of the whole pool, the
+    earlier tokens of a block whose scale grew among them, and an append enqueued twice."""
+    rng = np.random.default_rng(4)
+    pieces = [[1, 15, 16, 0], [1, 1, 3, 17], [7, 1, 40, 1], [1, 30, 1, 5], [100, 1, 1, 1], [1, 0, 1, 64]]
+    total = np.sum(pieces, axis=0)
+    whole = wl.custom_wave(4, 2, dim, dim, page, total * 0, total, seed=5, name="pieces")
+    t = make(whole, 6)
+    pools = [t["k_pool"].cuda(), t["v_pool"].cuda()]
+    want = [t["k_pool"].numpy(), t["v_pool"].numpy()]
+    prefix = np.zeros(4, dtype=np.int64)
+    for n, chunk in enumerate(pieces):
+        spec = wl.custom_wave(4, 2, dim, dim, page, prefix, chunk, seed=5, name="piece", num_pages=whole.num_pages)
+        spec.block_table = whole.block_table
+        size = np.exp(3.0 * rng.standard_normal((spec.total_tokens, 2, 1))).astype(np.float32)
+        new = [(torch.randn(spec.total_tokens, 2, dim, generator=torch.Generator().manual_seed(10 * n + i)) *
+                torch.from_numpy(size)).to(torch.bfloat16) for i in range(2)]
+        p = wp.q8_plan_for(spec)
+        ws = wp.new_workspace(p)
+        wp.plan_upload(p, ws)
+        want = [oracle.q8.append(w, wl.to_bits(x), prefix, chunk, whole.block_table, dim, page) for w, x in zip(want, new)]
+        for _ in range(2):
+            wp.q8_append_kv(p, *[x.cuda() for x in new], *pools, ws)
+            torch.cuda.synchronize()
+            for pool, w in zip(pools, want):
+                assert np.array_equal(pool.cpu().numpy(), w), n
+        prefix = prefix + chunk
+
+
+WAVES = {
+    # name: (q heads, KV heads, dim, page, prefix, chunk)
+    "one_token": (32, 8, 128, 64, [0], [1]),
+    "tokens": (32, 8, 128, 64, [700, 40, 0, 63, 64, 15], [1, 1, 1, 1, 1, 1]),
+    "tokens_small": (24, 4, 64, 16, [300, 15, 16, 0], [1, 1, 1, 1]),
+    "tokens_small_pages": (16, 2, 128, 16, [257, 31], [1, 1]),
+    "tokens_small_heads": (8, 8, 64, 64, [129, 31], [1, 1]),
+    "two_tiles_of_rows": (32, 1, 64, 64, [90, 400], [1, 1]),
+    "few_rows_mixed": (16, 2, 128, 64, [200, 31, 333], [4, 2, 3]),
+    "few_rows_16": (16, 2, 128, 16, [200, 31], [2, 1]),
+    "odd_group": (15, 3, 64, 16, [77, 5], [1, 6]),
+    "four_waves": (16, 2, 128, 64, [100, 0, 77], [9, 16, 1]),
+    "four_waves_small": (24, 4, 64, 16, [50, 3], [17, 21]),
+    "wide_group": (16, 1, 128, 64, [130], [7]),
+    "group_of_40": (40, 1, 64, 64, [70], [1]),
+    "eight_waves": (8, 2, 128, 64, [70, 0, 0], [150, 40, 65]),
+    "eight_waves_small": (8, 2, 64, 16, [33, 5], [130, 70]),
+    "chunks_beside_tokens": (8, 2, 128, 64, [70, 700, 0, 300, 2000, 0], [150, 1, 40, 8, 0, 1]),
+    "short_chunks_beside_tokens": (24, 4, 64, 16, [900, 50, 17], [1, 17, 5]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(WAVES))
+@pytest.mark.parametrize("splits", [0, 1, 3])
+def test_attention_against_the_oracle(name, splits):
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=11, name=name)
+    t = make(spec, 12)
+    check(spec, t, on_gpu(spec, t, max_splits=splits), f"splits {splits}")
+
+
+def score_forms(spec, rng):
+    """Scores of every form, and their mixtures."""
+    T = spec.total_tokens
+    pos = np.concatenate([p + np.arange(c) for p, c in zip(spec.prefix_lens, spec.chunk_lens)]).astype(np.int64)
+    n = np.repeat(spec.prefix_lens + spec.chunk_lens, spec.chunk_lens).astype(np.int64)
+    slopes = np.exp2(-8.0 * (1 + np.arange(spec.num_q_heads)) / spec.num_q_heads)
+    window = np.maximum(0, pos + 1 - 20)
+    start = np.maximum(0, pos - pos % 37)                                    # documents of 37 tokens
+    shared = np.minimum(n, np.maximum(pos + 1, start + 15))                  # whose first 15 tokens all of one sees
+    any_lo, any_hi = rng.integers(0, n + 1), rng.integers(0, n + 1)          # half of them empty
+    return {
+        "cap": {"cap": 2.0}, "wide_cap": {"cap": 500.0}, "slopes": {"slopes": slopes},
+        "window": {"key_begin": window}, "documents": {"key_begin": start},
+        "prefix": {"key_begin": start, "key_end": shared}, "all_keys": {"key_end": n},
+        "any": {"key_begin": any_lo, "key_end": any_hi}, "nothing": {"key_begin": pos + 1}, "nothing_at_all": {"key_end": pos * 0},
+        "first_key_alone": {"key_end": np.minimum(n, 1)}, "last_key_alone": {"key_begin": n - 1, "key_end": n},
+        "mixed": {"cap": 3.0, "slopes": slopes, "key_begin": any_lo, "key_end": any_hi},
+        "negative_slopes": {"cap": 5.0, "slopes": -0.01 * slopes, "key_end": n},
+    }
+
+
+FORMS = sorted(score_forms(wl.custom_wave(2, 1, 64, 64, 16, [1], [1], seed=0), np.random.default_rng(0)))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("name", ["tokens", "tokens_small", "two_tiles_of_rows", "few_rows_mixed", "odd_group", "four_waves",
+                                  "eight_waves", "eight_waves_small", "chunks_beside_tokens"])
+def test_scores_against_the_oracle(name, form):
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=41, name=name)
+    t = make(spec, 42)
+    s = score_forms(spec, np.random.default_rng(43))[form]
+    kw = {("score_cap" if n == "cap" else n): x for n, x in s.items()}
+    for splits in (0, 3):
+        check(spec, t, on_gpu(spec, t, max_splits=splits, **kw), f"{form} splits {splits}", **s)
+
+
+@pytest.mark.parametrize("name", ["tokens", "few_rows_mixed", "four_waves", "eight_waves"])
+def test_the_causal_rule_spelled_out_is_the_plain_one(name):
+    """Intervals that say what the plain plan means leave the same keys: the same answers but for the order of a sum."""
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=44, name=name)
+    t = make(spec, 45)
+    pos = np.concatenate([p + np.arange(c) for p, c in zip(prefix, chunk)])
+    check(spec, t, on_gpu(spec, t, key_begin=pos * 0, key_end=pos + 1), "spelled out")
+
+
+@pytest.mark.parametrize("q,kv,dim,page", [(64, 8, 128, 64), (24, 4, 64, 16)])
+def test_long_cache_and_many_splits(q, kv, dim, page):
+    spec = wl.custom_wave(q, kv, dim, dim, page, [9000, 2049], [1, 1], seed=13, name=f"long_{dim}")
+    t = make(spec, 14)
+    g = on_gpu(spec, t)
+    assert g["plan"].info()["max_splits"] > 4
+    check(spec, t, g)
+    s = {"key_begin": np.array([4500, 100]), "key_end": np.array([8190, 100])}       # a window, and a row that sees nothing
+    g = on_gpu(spec, t, **s)
+    check(spec, t, g, "window", **s)
+
+
+@pytest.mark.parametrize("scale", [30.0, 1e-3])
+def test_large_and_small_logits(scale):
+    """The running maximum moves by far more than its slack, and back."""
+    spec = wl.custom_wave(16, 2, 128, 128, 64, [300, 400], [1, 30], seed=15, name="needle")
+    t = make(spec, 16)
+    t["q"] = (t["q"].float() * scale).to(torch.bfloat16)
+    check(spec, t, on_gpu(spec, t), f"x {scale}")
+    check(spec, t, on_gpu(spec, t, score_cap=20.0), f"x {scale}, capped", cap=20.0)
+
+
+def test_stale_slots_and_later_tokens_do_not_leak():
+    """Bytes behind the last token, and what a later token of the chunk holds (NaN, infinities), leave a row as it is but for
+    its block's scale."""
+    for name in ("few_rows_mixed", "four_waves", "eight_waves"):
+        q, kv, dim, page, prefix, chunk = WAVES[name]
+        spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=17, name=name)
+        t = make(spec, 18)
+        a = on_gpu(spec, t)
+        other = make(spec, 18, garbage=False)
+        b = on_gpu(spec, {**t, **{n: other[n] for n in ("k_pool", "v_pool")}})
+        assert same(a["out"], b["out"]) and same(a["lse"], b["lse"])
+        # the request's last token, moved into a block of its own
+        chunk2 = [c + (-(p + c) % 16) + 1 if i == 0 else c for i, (p, c) in enumerate(zip(prefix, chunk))]
+        spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk2, seed=17, name=name)
+        t = make(spec, 19)
+        a = on_gpu(spec, t)
+        end = chunk2[0] - 1
+        bad = {n: x.clone() for n, x in t.items()}
+        bad["k_new"][end], bad["v_new"][end] = float("nan"), float("inf")
+        c = on_gpu(spec, bad)
+        keep = np.arange(spec.total_tokens) != end
+        assert same(a["out"][keep], c["out"][keep]) and same(a["lse"][keep], c["lse"][keep])
+        assert not (c["out"][end].float().abs() < 1e30).any(), "a row that sees the bad token shows it"
+        # masked away by intervals, the bad token is as if it were not there
+        pos = np.concatenate([p + np.arange(n) for p, n in zip(prefix, chunk2)])
+        hide = {"key_end": np.where(keep, pos + 1, pos)}
+        x, y = on_gpu(spec, t, **hide), on_gpu(spec, bad, **hide)
+        assert same(x["out"], y["out"]) and same(x["lse"], y["lse"])
+
+
+def test_a_query_of_nan_and_a_score_that_overflows_show():
+    for name in ("tokens", "few_rows_mixed", "four_waves", "eight_waves"):
+        q, kv, dim, page, prefix, chunk = WAVES[name]
+        spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=51, name=name)
+        t = make(spec, 52)
+        t["q"] = t["q"].abs()
+        for splits in (1, 3):
+            clean = on_gpu(spec, t, max_splits=splits)
+            bad = {n: x.clone() for n, x in t.items()}
+            bad["q"][0] = float("nan")
+            g = on_gpu(spec, bad, max_splits=splits)
+            assert torch.isnan(g["out"][0].float()).all() and torch.isnan(g["lse"][0]).all()
+            assert same(g["out"][1:], clean["out"][1:]) and same(g["lse"][1:], clean["lse"][1:])
+            bad = {n: x.clone() for n, x in t.items()}
+            bad["k_new"][0] = float("inf")                       # the largest magnitude in every place
+            g = on_gpu(spec, bad, max_splits=splits)
+            seen = slice(0, chunk[0])
+            assert torch.isnan(g["lse"][seen]).all() and torch.isnan(g["out"][seen].float()).all()
+            # under a cap that score is the cap, and nothing else
+            g = on_gpu(spec, bad, max_splits=splits, score_cap=4.0)
+            assert torch.isfinite(g["lse"]).all()
+            check(spec, bad, g, "capped", cap=4.0) if name == "tokens" else None
+
+
+def test_repeated_calls_and_page_orders_are_bit_identical():
+    spec = wl.custom_wave(64, 8, 128, 128, 64, [1500, 700, 64], [1, 1, 1], seed=19, name="repeat")
+    t = make(spec, 20)
+    a, b = on_gpu(spec, t), on_gpu(spec, t)
+    assert a["plan"].info()["max_splits"] > 1
+    assert same(a["out"], b["out"])
+    perm = np.random.default_rng(21).permutation(spec.num_pages).astype(np.int32)
+    moved = {**t, **{n: torch.empty_like(t[n]) for n in ("k_pool", "v_pool")}}
+    for n in ("k_pool", "v_pool"):
+        moved[n][perm] = t[n]
+    other = wl.custom_wave(64, 8, 128, 128, 64, [1500, 700, 64], [1, 1, 1], seed=19, name="repeat")
+    other.block_table = np.where(other.block_table >= 0, perm[np.maximum(other.block_table, 0)], -1).astype(np.int32)
+    c = on_gpu(other, moved)
+    assert same(a["out"], c["out"]) and same(a["lse"], c["lse"])
+
+
+def test_shared_prefix_pages():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [64, 64, 64], [1, 2, 1], seed=22, shared_prefix_pages=3, name="shared")
+    t = make(spec, 23)
+    check(spec, t, on_gpu(spec, t))
+
+
+def test_graph_replays_match_eager():
+    """Append and attention captured once, with scores, and replayed with new inputs in the same buffers, eager work between."""
+    spec = wl.custom_wave(64, 8, 128, 128, 64, [3000, 130, 5], [1, 1, 1], seed=24, name="graph")
+    scores = {"score_cap": 30.0, "slopes": np.full(64, 0.01), "key_begin": [100, 0, 2]}
+    t = [make(spec, 25 + i) for i in range(3)]
+    eager = [on_gpu(spec, x, **scores) for x in t]
+    p = eager[0]["plan"]
+    assert p.info()["num_merge_items"] > 0
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    buf = {n: x.cuda() for n, x in t[0].items()}
+    out, lse = torch.empty_like(eager[0]["out"]), torch.empty_like(eager[0]["lse"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        wp.q8_append_kv(p, buf["k_new"], buf["v_new"], buf["k_pool"], buf["v_pool"], ws)
+        wp.q8_chunked_prefill(p, buf["q"], buf["k_pool"], buf["v_pool"], out, lse, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert same(out, eager[0]["out"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        wp.q8_append_kv(p, buf["k_new"], buf["v_new"], buf["k_pool"], buf["v_pool"], ws)
+        wp.q8_chunked_prefill(p, buf["q"], buf["k_pool"], buf["v_pool"], out, lse, ws)
+    for i in (0, 1, 2, 1):
+        for n, x in t[i].items():
+            buf[n].copy_(x)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("out", "lse", "k_pool", "v_pool"):
+            assert same({"out": out, "lse": lse, **buf}[n], eager[i][n]), (i, n)
+
+
+def test_two_plans_on_two_streams():
+    specs = [wl.custom_wave(64, 8, 128, 128, 64, [2500 + 100 * i, 40], [1, 2], seed=30 + i, name=f"stream{i}") for i in range(2)]
+    t = [make(s, 32 + i) for i, s in enumerate(specs)]
+    want = [on_gpu(s, x, score_cap=10.0 * i) for i, (s, x) in enumerate(zip(specs, t))]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for i in range(2):
+            w = want[i]
+            with torch.cuda.stream(streams[i]):
+                out, lse = torch.empty_like(w["out"]), torch.empty_like(w["lse"])
+                wp.q8_chunked_prefill(w["plan"], w["q"], w["k_pool"], w["v_pool"], out, lse, w["ws"])
+                got.append(out)
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert same(got[i], want[i]["out"])
+
+
+def test_lse_is_optional_and_idle_waves_do_nothing():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [1, 3], seed=26, name="no_lse")
+    t = make(spec, 27)
+    g = on_gpu(spec, t)
+    out = torch.empty_like(g["out"])
+    wp.q8_chunked_prefill(g["plan"], g["q"], g["k_pool"], g["v_pool"], out, None, g["ws"])
+    assert same(out, g["out"])
+    idle = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [0, 0], seed=28, name="idle")
+    t = make(idle, 29)
+    for kw in ({}, {"key_begin": [], "key_end": []}):
+        g = on_gpu(idle, t, **kw)
+        assert g["out"].shape[0] == 0 and torch.equal(g["k_pool"].cpu(), t["k_pool"])
+
+
+def test_a_workspace_overwritten_since_its_upload_writes_nothing():
+    spec = wl.custom_wave(8, 2, 64, 64, 16, [40, 20], [1, 3], seed=26, name="stale")
+    t = make(spec, 27)
+    g = on_gpu(spec, t)
+    ws = torch.zeros_like(g["ws"])
+    wp.plan_upload(g["plan"], ws)
+    ws.zero_()
+    out, before = torch.zeros_like(g["out"]), g["k_pool"].clone()
+    wp.q8_append_kv(g["plan"], g["v_new"], g["k_new"], g["k_pool"], g["v_pool"], ws)
+    wp.q8_chunked_prefill(g["plan"], g["q"], g["k_pool"], g["v_pool"], out, None, ws)
+    assert not out.view(torch.int16).any() and torch.equal(before, g["k_pool"])
+
+
+def test_byte_offsets_past_32_bits():
+    """Pages at the far end of pools of more than 4 GiB, written, read back and attended to."""
+    P = (1 << 32) // (8 * (64 * 128 + 16)) + 40
+    spec = wl.custom_wave(16, 8, 128, 128, 64, [130, 700], [1, 40], seed=61, name="wide", num_pages=24)
+    t = make(spec, 62)
+    near = on_gpu(spec, t)
+    far = wl.custom_wave(16, 8, 128, 128, 64, [130, 700], [1, 40], seed=61, name="wide", num_pages=24)
+    far.num_pages, far.block_table = P, np.where(spec.block_table >= 0, spec.block_table + P - 24, -1).astype(np.int32)
+    p = wp.q8_plan_for(far)
+    ws = wp.new_workspace(p)
+    wp.plan_upload(p, ws)
+    pools = []
+    for n in ("k_pool", "v_pool"):
+        pool = torch.empty(P, 8, 64 * 128 + 16, dtype=torch.uint8, device="cuda")
+        pool[P - 24:] = t[n].cuda()
+        pools.append(pool)
+    out, lse = torch.empty_like(near["out"]), torch.empty_like(near["lse"])
+    wp.q8_append_kv(p, near["k_new"], near["v_new"], *pools, ws)
+    wp.q8_chunked_prefill(p, near["q"], *pools, out, lse, ws)
+    back = [torch.empty_like(near["k_new"]) for _ in range(4)]
+    wp.q8_read_kv(p, *pools, *back[:2], ws)
+    wp.q8_read_kv(near["plan"], near["k_pool"], near["v_pool"], *back[2:], near["ws"])
+    torch.cuda.synchronize()
+    assert same(out, near["out"]) and same(lse, near["lse"])
+    assert same(back[0], back[2]) and same(back[1], back[3])
+    for n, pool in zip(("k_pool", "v_pool"), pools):
+        assert same(pool[P - 24:], near[n])
