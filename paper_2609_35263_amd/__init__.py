@@ -772,33 +772,41 @@ def _row_args(here, name, t, shape, dtype):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the plan needs {shape}")
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    s = t.stride()
-    if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
-        raise ValueError(f"{name} must be contiguous within a token, its strides are {s}")
-    return t.data_ptr(), s[0] if shape[0] > 1 else shape[1] * shape[2]
+    width = shape[1] * shape[2]
+    if shape[0] <= 1 or t.is_contiguous():
+        step = width
+    else:
+        step = t.stride(0)
+    if step != width or not t.is_contiguous():
+        s = t.stride()
+        if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
+            raise ValueError(f"{name} must be contiguous within a token, its strides are {s}")
+    return t.data_ptr(), step
 
 
 def rope_apply(rope: Rope, p: Plan, q, k, q_out, k_out, workspace, positions=None, stream=None):
     """Turn the query and key rows of the plan's new tokens by their positions (or by positions, int32 [T] on the device).
     q_out is q, or a tensor apart from all others; so with k, and either pair may be None.  Tokens may lie apart, as in slices of
     one packed projection."""
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None):
+        raise ValueError("q and q_out, and k and k_out, come together")
     import torch
+    bf = torch.bfloat16
     here = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
-    sh = _attn_shapes(p)
-    for name, t, t_out in (("q", q, q_out), ("k", k, k_out)):
-        if (t is None) != (t_out is None):
-            raise ValueError(f"{name} and {name}_out come together")
-    args = []
-    for name, t, t_out, shape in (("q", q, q_out, sh["q"]), ("k", k, k_out, sh["k_new"])):
-        args.append((None, 0, None, 0) if t is None else (*_row_args(here, name, t, shape, torch.bfloat16),
-                                                         *_row_args(here, name + "_out", t_out, shape, torch.bfloat16)))
-    bufs = [("workspace", workspace, None, None)]
-    if positions is not None:
-        bufs.append(("positions", positions, (sh["q"][0],), torch.int32))
-    ws, *at, st = _call_args(stream, *bufs)
-    (q_at, q_s, qo_at, qo_s), (k_at, k_s, ko_at, ko_s) = args
-    _check(load_library().wavepp_rope_apply(rope.handle, p.handle, q_at, q_s, k_at, k_s, qo_at, qo_s, ko_at, ko_s,
-                                            at[0] if at else None, ws, workspace.nbytes, st))
+    sh = p._buffers or _attn_shapes(p)
+    q_at = q_step = qo_at = qo_step = k_at = k_step = ko_at = ko_step = at = None
+    if q is not None:
+        q_at, q_step = _row_args(here, "q", q, sh["q"], bf)
+        qo_at, qo_step = (q_at, q_step) if q_out is q else _row_args(here, "q_out", q_out, sh["q"], bf)
+    if k is not None:
+        k_at, k_step = _row_args(here, "k", k, sh["k_new"], bf)
+        ko_at, ko_step = (k_at, k_step) if k_out is k else _row_args(here, "k_out", k_out, sh["k_new"], bf)
+    if positions is None:
+        ws, st = _call_args(stream, ("workspace", workspace, None, None))
+    else:
+        ws, at, st = _call_args(stream, ("workspace", workspace, None, None), ("positions", positions, sh["q"][:1], torch.int32))
+    _check(load_library().wavepp_rope_apply(rope.handle, p.handle, q_at, q_step or 0, k_at, k_step or 0, qo_at, qo_step or 0,
+                                            ko_at, ko_step or 0, at, ws, workspace.nbytes, st))
 
 
 # ------------------------------------------------------------------------------------------------

@@ -792,7 +792,7 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     else max_rows = std::max(max_rows, rows_of(r));
   }
   const bool any_many = max_rows > 0;
-  const bool small_rows = gw_n == 4 || (gw_n != 8 && max_rows <= kGqaRowsPerItem / 2);
+  bool small_rows = gw_n == 4 || (gw_n != 8 && max_rows <= kGqaRowsPerItem / 2);
   std::vector<ReqMeta> reqs(R);
   int64_t cu = 0;
   for (int32_t r = 0; r < R; ++r) {
@@ -820,6 +820,37 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
                           scores->key_end ? scores->key_end[t] : batch->prefix_lens[r] + i + 1});
       }
   }
+  // Keys of the M rows from r0 on, from a tile's first: all that one of their tokens sees.
+  auto tile_keys = [&](int32_t r, int64_t r0, int64_t M, int64_t KT) {
+    const int64_t first = r0 / G, last = (std::min<int64_t>(r0 + M, rows_of(r)) - 1) / G;
+    if (!ranged) return TokenRange{0, int32_t(batch->prefix_lens[r] + last + 1)};
+    TokenRange u{INT32_MAX, 0};
+    for (int64_t t = first; t <= last; ++t) {
+      const TokenRange& x = ranges[size_t(reqs[r].cu + t)];
+      if (x.begin < x.end) u = {std::min(u.begin, x.begin), std::max(u.end, x.end)};
+    }
+    return u.begin < u.end ? TokenRange{int32_t(u.begin / KT * KT), u.end} : TokenRange{0, 0};
+  };
+  // Over 8-bit pages, items of few keys also run in the 4-wave form, two workgroups a CU, whose prologues, barriers and
+  // diagonals fall beside the other's products; long ones lose more by turning each tile into bf16 for half of the rows.
+  // With mean keys an item of (us with 8 waves, with 4), 32/8 heads of 128: 300 137, 126; 800 243, 237; 1,250 181, 175;
+  // 2,000 656, 700; 3,100 483, 522.  With capped scores, whose vector work weighs more: 300 187, 142; 1,250 226, 204; 3,100
+  // 624, 618; 66,000 2,552, 2,687.  24/4 heads of 64: 800 119, 98; 1,250 89, 80; 3,100 250, 243, capped 325, 303.  Where that leaves
+  // too few items for the chip, key ranges would be cut instead: 8 waves.
+  if (cache == Cache::q8 && gw_n == 0 && any_many && !small_rows) {
+    int64_t items = 0, tiles = 0, keys = 0;
+    for (int32_t r = 0; r < R; ++r) {
+      if (is_few(r)) continue;
+      const int64_t rows = rows_of(r);
+      items += ceil_div(rows, kGqaRowsPerItem / 2) * s.num_kv_heads;
+      for (int64_t r0 = 0; r0 < rows; r0 += kGqaRowsPerItem, ++tiles) {
+        const TokenRange k = tile_keys(r, r0, kGqaRowsPerItem, kKvTile);
+        keys += k.end - k.begin;
+      }
+    }
+    const int64_t most = (scores && scores->cap > 0.0f ? 4096 : 1536) * (128 / s.head_dim_qk);
+    small_rows = items >= 2 * kNumCu && keys <= most * tiles;
+  }
   int64_t part_rows = 0;
   int max_used = 1;
 
@@ -838,18 +869,10 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     std::vector<TokenRange> seen;
     for (int32_t r = 0; r < R; ++r) {
       if (is_few(r) != few_rows) continue;
-      const int32_t p = batch->prefix_lens[r];
       const int64_t rows_total = rows_of(r);
       if (few_rows) plan->few_rows = std::max(plan->few_rows, int32_t(rows_total));
       seen.clear();
-      for (int64_t r0 = 0; ranged && r0 < rows_total; r0 += M) {
-        TokenRange u{INT32_MAX, 0};                 // all keys of the tile's tokens, from a tile's first
-        for (int64_t t = r0 / G; t <= (std::min<int64_t>(r0 + M, rows_total) - 1) / G; ++t) {
-          const TokenRange& x = ranges[size_t(reqs[r].cu + t)];
-          if (x.begin < x.end) u = {std::min(u.begin, x.begin), std::max(u.end, x.end)};
-        }
-        seen.push_back(u.begin < u.end ? TokenRange{u.begin / KT * KT, u.end} : TokenRange{0, 0});
-      }
+      for (int64_t r0 = 0; r0 < rows_total; r0 += M) seen.push_back(tile_keys(r, r0, M, KT));
       for (int32_t g = 0; g < s.num_kv_heads; ++g)
         for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
           WorkItem w{};
@@ -857,9 +880,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
           w.kv_head = g;
           w.row0 = int32_t(r0);
           w.rows = int32_t(std::min<int64_t>(M, rows_total - r0));
-          const int64_t last_tok = (r0 + w.rows - 1) / G;
-          w.kv_begin = ranged ? seen[size_t(r0 / M)].begin : 0;
-          w.kv_end = ranged ? seen[size_t(r0 / M)].end : int32_t(p + last_tok + 1);
+          w.kv_begin = seen[size_t(r0 / M)].begin;
+          w.kv_end = seen[size_t(r0 / M)].end;
           w.part = -1;
           w.split = 0;
           base.push_back(w);
@@ -1041,6 +1063,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     plan->num_blocks = int32_t(blocks.size());
     plan->off_blocks = off;
     off = align_up(off + sizeof(Q8Block) * blocks.size(), 16);
+    plan->off_item_reqs = off;
+    off = align_up(off + sizeof(ReqMeta) * plan->items.size(), 16);
     if (ranged) {
       plan->off_ranges = off;
       off = align_up(off + sizeof(TokenRange) * ranges.size(), 16);
@@ -1069,6 +1093,13 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   if (!plan->merges.empty())
     memcpy(plan->blob.data() + plan->off_merges, plan->merges.data(), sizeof(MergeItem) * plan->merges.size());
   if (!blocks.empty()) memcpy(plan->blob.data() + plan->off_blocks, blocks.data(), sizeof(Q8Block) * blocks.size());
+  if (plan->off_item_reqs) {
+    unsigned char* at = plan->blob.data() + plan->off_item_reqs;
+    for (const WorkItem& w : plan->items) {
+      if (w.rows > 0) memcpy(at, &reqs[size_t(w.req)], sizeof(ReqMeta));      // (an item of padding has none)
+      at += sizeof(ReqMeta);
+    }
+  }
   if (plan->off_ranges && total)
     memcpy(plan->blob.data() + plan->off_ranges, ranges.data(), sizeof(TokenRange) * ranges.size());
   if (plan->off_slopes)

@@ -40,8 +40,8 @@ struct wavepp_plan {
   // metadata blob (uploaded as is) and its sub-array offsets
   std::vector<unsigned char> blob;
   size_t off_reqs = 0, off_bt = 0, off_items = 0, off_merges = 0;
-  // 8-bit pages: the blocks that the wave's tokens touch; the scores' arrays, 0 where the plan has none
-  size_t off_blocks = 0, off_ranges = 0, off_slopes = 0;
+  // 8-bit pages: the blocks that the wave's tokens touch, every item's request; the scores' arrays, 0 where the plan has none
+  size_t off_blocks = 0, off_item_reqs = 0, off_ranges = 0, off_slopes = 0;
   int32_t num_blocks = 0;
   float cap = 0.0f;
   size_t meta_bytes = 0;       // blob size rounded up to 256

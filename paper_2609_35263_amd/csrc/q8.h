@@ -25,6 +25,7 @@ struct alignas(16) Q8Block {
 // What the 8-bit cache's launches need beyond a DevPlan.
 struct Q8Dev {
   const Q8Block* blocks;
+  const ReqMeta* item_reqs;    // of every work item
   int32_t num_blocks;
   int32_t few_rows;            // most rows of an item that runs with few rows
   const TokenRange* ranges;    // of every new token; NULL: causal

@@ -87,10 +87,9 @@ template <int D>
 __global__ __launch_bounds__(256) void q8_append_kernel(DevPlan p, Q8Dev x, const u32x4* __restrict__ k_new,
                                                         const u32x4* __restrict__ v_new, uint8_t* __restrict__ k_pool,
                                                         uint8_t* __restrict__ v_pool) {
-  if (!meta_ok(p)) return;
   constexpr int LPR = D / 8, RPP = 64 / LPR, NP = kQ8Block / RPP;      // lanes of a row, rows a pass, passes
-  const BlockPart u = block_part(p, x);
-  if (!u.any) return;
+  const BlockPart u = block_part(p, x);          // in one trip with the header
+  if (int(!meta_ok(p)) | int(!u.any) | int(u.lo >= u.hi)) return;
   const int Hkv = p.num_kv_heads, B = p.page_size, lane = threadIdx.x & 63, first = lane / LPR;
   const u32x4* rows = (u.is_v ? v_new : k_new) + (int64_t(u.b.token) * Hkv + u.head) * LPR + lane % LPR;
   uint8_t* run = (u.is_v ? v_pool : k_pool) + (int64_t(u.b.page) * Hkv + u.head) * (B * D + kQ8ScaleBytes);
@@ -143,10 +142,9 @@ template <int D>
 __global__ __launch_bounds__(256) void q8_read_kernel(DevPlan p, Q8Dev x, const uint8_t* __restrict__ k_pool,
                                                       const uint8_t* __restrict__ v_pool, bf16x8* __restrict__ k_out,
                                                       bf16x8* __restrict__ v_out) {
-  if (!meta_ok(p)) return;
   constexpr int LPR = D / 8, RPP = 64 / LPR, NP = kQ8Block / RPP;
-  const BlockPart u = block_part(p, x);
-  if (!u.any) return;
+  const BlockPart u = block_part(p, x);          // in one trip with the header
+  if (int(!meta_ok(p)) | int(!u.any) | int(u.lo >= u.hi)) return;
   const int Hkv = p.num_kv_heads, B = p.page_size, lane = threadIdx.x & 63, first = lane / LPR;
   const uint8_t* run = (u.is_v ? v_pool : k_pool) + (int64_t(u.b.page) * Hkv + u.head) * (B * D + kQ8ScaleBytes);
   const uint8_t* codes = run + (u.b.slot + first) * D + 8 * (lane % LPR);
@@ -175,33 +173,55 @@ __device__ __forceinline__ float reference(float m) { return m < -kFarScore ? 0.
 // The sum that a row's outputs are divided by: 0 for a row of no weight, NaN for one that has no sum.
 __device__ __forceinline__ float row_sum(float m, float l) { return m <= kFarScore ? l : NAN; }
 
-// Scores other than softmax_scale q.k of one lane's query row.  |i - j| of key j = base + c is |from - c|.
-struct RowScores {
-  float in, out;               // the cap's factors
-  float slope;                 // times log2 e
-  bool capped, wide, sloped;
+// What a kernel's scores are.  CAUSAL: softmax_scale q.k up to the row's own position.  LINEAR: with a slope on the distance, or
+// an interval of keys.  CAPPED: with a cap of kFixedCap at most, and perhaps an interval.  MIXED: with a cap otherwise.
+enum Form { CAUSAL, LINEAR, CAPPED, MIXED };
+
+// Scores of CAPPED lie within c = cap log2 e of 0, so their weights need no running reference: they are taken against one fixed
+// at min(c, 80 - c), which leaves them within 2^-80 and 2^(2 c - 80), sums and products with values up to 2^40 far inside fp32.
+constexpr float kFixedCap = 55.0f;
+
+// One lane's query row's scores.  A product's accumulator becomes a value x whose score is a x + b, so the weight is one fused
+// multiply-add and one exp2 of x in every form:
+//   * x = q.k less the slope over softmax_scale times the distance, a = softmax_scale log2 e; or
+//   * x = -1 / (1 + e^2z), z = softmax_scale q.k / cap, a = 2 cap log2 e and b = cap log2 e, as tanh z = 1 - 2 / (1 + e^2z):
+//     good to 2^-21 at all z, for a multiply, an addition, and an instruction of lower rate for each of exp2 and the reciprocal
+//     (CAPPED); or
+//   * the score itself (MIXED).  A cap over 128 multiplies that error beyond a score's own rounding: small z then take the
+//     series, whose next term is 2^-26 of z at a quarter.
+struct Scores {
+  float a, b;
+  float in, out;               // CAPPED: 2 log2 e softmax_scale / cap, cap log2 e
+  float slope;                 // over softmax_scale where LINEAR, times log2 e where MIXED
+  bool sloped, wide;
 };
-__device__ __forceinline__ RowScores row_scores(const DevPlan& p, const Q8Dev& x, int head) {
-  RowScores r{};
-  r.capped = x.cap > 0.0f;
-  if (r.capped) {
-    r.in = p.softmax_scale / x.cap;
+template <Form F>
+__device__ __forceinline__ Scores scores_of(const DevPlan& p, const Q8Dev& x, int head) {
+  Scores r{};
+  r.a = p.softmax_scale * kLog2e;
+  r.sloped = F != CAUSAL && x.slopes;
+  if (r.sloped) r.slope = x.slopes[head] * (F == MIXED ? kLog2e : 1.0f / p.softmax_scale);
+  if (F == CAPPED || F == MIXED) {
+    r.in = 2.0f * kLog2e * p.softmax_scale / x.cap;
     r.out = x.cap * kLog2e;
     r.wide = x.cap > 128.0f;
+    r.a = F == MIXED ? 1.0f : 2.0f * r.out;
+    r.b = F == MIXED ? 0.0f : r.out;
   }
-  r.sloped = x.slopes != nullptr;
-  if (r.sloped) r.slope = x.slopes[head] * kLog2e;
   return r;
 }
-// tanh(z) = 1 - 2 / (1 + e^2z), good to 2^-21 at all z: an instruction of quarter rate for each of exp2 and the reciprocal.
-// A cap over 128 multiplies that beyond a score's own rounding, so small z then take the series, whose next term is
-// 2^-26 of z at a quarter.
-__device__ __forceinline__ float tanh_of(float z, bool wide) {
-  const float t = 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + fast_exp2(2.0f * kLog2e * z));
-  if (!wide) return t;
-  const float y = z * z;
+__device__ __forceinline__ float fixed_reference(const Scores& r) { return fminf(r.out, 80.0f - r.out); }
+// -1 / (1 + e^2z) of a product.
+__device__ __forceinline__ float logistic_of(float s, const Scores& r) {
+  return __builtin_amdgcn_rcpf(-1.0f - fast_exp2(s * r.in));
+}
+// cap log2 e tanh z of a product.
+__device__ __forceinline__ float capped_of(float s, const Scores& r) {
+  const float t = fmaf(2.0f, logistic_of(s, r), 1.0f);
+  if (!r.wide) return r.out * t;
+  const float z = s * r.in * (0.5f * kLn2), y = z * z;
   const float series = z * (1.0f + y * (-0x1.555556p-2f + y * (0x1.111112p-3f + y * (-0x1.ba1ba2p-5f + y * 0x1.664f48p-6f))));
-  return fabsf(z) < 0.25f ? series : t;
+  return r.out * (fabsf(z) < 0.25f ? series : t);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -218,7 +238,7 @@ __device__ __forceinline__ float tanh_of(float z, bool wide) {
 // on distinct banks.
 __device__ __forceinline__ int v_place(int c) { return 8 * (c ^ ((c >> 2) & 3)); }
 
-template <int D, int NW, bool PLAIN>
+template <int D, int NW, Form F>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPlan p, Q8Dev x, const __bf16* __restrict__ q,
                                                                            const uint8_t* __restrict__ kpool,
                                                                            const uint8_t* __restrict__ vpool,
@@ -229,14 +249,15 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   constexpr int KSTR = D + 8;          // K rows in LDS: 16-byte reads of 8 rows land on distinct banks
   constexpr int VSTR = D + 32;         // V rows: transposed reads of 4 rows x 2 groups x 32 bytes on distinct banks
   constexpr int W = D / 64;            // 16-byte pieces of codes per thread and tile, for K and for V: a quarter of a row
+  constexpr int AHEAD = 2;             // CAPPED: LDS reads ahead of their products
   static_assert(KT * 4 == NW * 64, "four threads a key, 16 keys a wave");
   __shared__ __attribute__((aligned(16))) __bf16 ks[2][KT * KSTR];
   __shared__ __attribute__((aligned(16))) __bf16 vs[2][KT * VSTR];
 
-  if (!meta_ok(p)) return;
+  // the header, the item and its request in one trip to memory
   const WorkItem it = p.items[blockIdx.x];
-  if (it.rows <= 0) return;
-  const ReqMeta rm = p.reqs[it.req];
+  const ReqMeta rm = x.item_reqs[blockIdx.x];
+  if (int(!meta_ok(p)) | int(it.rows <= 0) | int(rm.chunk <= 0)) return;
   const int Hq = p.num_q_heads, Hkv = p.num_kv_heads;
   const int G = Hq / Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hf = lane >> 5;
@@ -255,7 +276,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   const int tok = prow / G;
   const int head = it.kv_head * G + (prow - tok * G);
   int begin = 0, end = rm.prefix + tok + 1;                      // keys that this row sees
-  if (!PLAIN && x.ranges) {
+  if (F != CAUSAL && x.ranges) {
     const TokenRange seen = x.ranges[rm.cu + tok];
     begin = seen.begin;
     end = seen.end;
@@ -272,9 +293,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   // Tiles in [wave_first, wave_end) have keys that a row of the wave sees; all rows see all keys of [all_first, all_end).
   int wave_first = 0, wave_end = rm.prefix + (it.row0 + max(wrow_last, wrow0)) / G + 1;
   int all_first = 0, all_end = rm.prefix + (it.row0 + wrow0) / G + 1;
-  RowScores sc{};
-  if (!PLAIN) {
-    sc = row_scores(p, x, head);
+  const Scores sc = scores_of<F>(p, x, head);
+  if (F != CAUSAL) {
     if (x.ranges) {
       wave_first = row_ok && begin < end ? begin : INT32_MAX;
       wave_end = row_ok && begin < end ? end : 0;
@@ -297,8 +317,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   f32x16 oacc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
-  float m_run = -INFINITY, l_run = 0.0f;
-  const float sl2 = p.softmax_scale * kLog2e;
+  float m_run = F == CAPPED ? fixed_reference(sc) : -INFINITY, l_run = 0.0f;      // CAPPED: l_run is of half of the keys
 
   // ---- K/V tile staging -----------------------------------------------------------------------
   // Thread tid has a quarter of key tid / 4's row.  Positions past the request's last valid one are clamped to that
@@ -344,6 +363,104 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
     v_lane[db] = (4 * hf + (lane & 15) / 4) * VSTR + v_place(4 * db + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) +
                  4 * (lane & 1);
 
+  // A tile of CAPPED scores: with the reference fixed, nothing waits for a maximum, so the weights of one block of 32 keys are
+  // worked out behind the products of the next one's scores and those of the last one's weights with V: an element of them
+  // after each product.  The order is pinned: left to itself the compiler makes blocks of each.
+  auto capped_tile = [&](int buf) {
+    constexpr int M = D / 16;                    // products of a block's scores, and of its weights with V
+    const float less = sc.b - m_run;
+    const __bf16* kl = &ks[buf][k_lane];
+    const __bf16* vl = &vs[buf][0];
+    auto k_read = [&](int n) { return *reinterpret_cast<const bf16x8*>(kl + 32 * (n / M) * KSTR + 16 * (n % M)); };
+    auto v_read = [&](int n) {                   // product n of a tile with V: step n / (D / 32), columns n % (D / 32)
+      const __bf16* at = vl + v_lane[n % (D / 32)] + 16 * (n / (D / 32)) * VSTR;
+      const bf16x4 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * VSTR);
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    f32x16 s = f32x16{}, next = f32x16{};
+    bf16x8 kf[AHEAD], vf[AHEAD], pb[2];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) kf[i] = k_read(i);
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], qf[i], s, 0, 0, 0);
+      kf[i % AHEAD] = k_read(i + AHEAD);
+    }
+    // An element's weight is worked out in three parts, each behind the next product, so that no part waits for the one before.
+    float one = 0.0f, two = 0.0f, e = 0.0f;
+#pragma unroll
+    for (int kb = 0; kb <= NKB; ++kb) {
+      const bool scores = kb + 1 < NKB, weights = kb < NKB, values = kb > 0;
+      if (values)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) vf[i] = v_read((kb - 1) * M + i);
+      next = f32x16{};
+      bf16x8 pb_next[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int per = 16 / M;              // elements of the weights for each product of a kind
+        if (i % per == 0) {
+          const int n = i / per;
+          if (scores) {
+            next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[n % AHEAD], qf[n], next, 0, 0, 0);
+            if ((kb + 1) * M + n + AHEAD < NKB * M) kf[n % AHEAD] = k_read((kb + 1) * M + n + AHEAD);
+          }
+        }
+        const bool third = weights ? i >= 2 || kb > 0 : i < 2, second = weights ? i >= 1 || kb > 0 : i < 1;
+        if (third) {
+          e = fast_exp2(fmaf(two, sc.a, less));
+          l_run += e;
+          const int at = (i + 14) % 16;
+          if (i >= 2) pb_next[at >> 3][at & 7] = static_cast<__bf16>(e);
+          else pb[at >> 3][at & 7] = static_cast<__bf16>(e);
+        }
+        if (second) two = __builtin_amdgcn_rcpf(-1.0f - one);
+        if (weights) one = fast_exp2(s[i] * sc.in);
+        if (values && i % per == per - 1) {
+          const int n = i / per, db = n % (D / 32);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[n % AHEAD], pb[n / (D / 32)], oacc[db], 0, 0, 0);
+          if (n + AHEAD < M) vf[n % AHEAD] = v_read((kb - 1) * M + n + AHEAD);
+        }
+      }
+      s = next;
+      pb[0] = pb_next[0];
+      pb[1] = pb_next[1];
+    }
+  };
+
+  // The same with a mask, block by block: a tile at the end of what a row sees.
+  auto capped_edge = [&](int buf, int over, int under) {
+    const float less = sc.b - m_run;
+#pragma unroll 1
+    for (int kb = 0; kb < NKB; ++kb) {
+      const __bf16* kl = &ks[buf][k_lane + 32 * kb * KSTR];
+      const __bf16* vl = &vs[buf][32 * kb * VSTR];
+      f32x16 s = f32x16{};
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kl + 16 * i), qf[i], s, 0, 0, 0);
+      bf16x8 pb[2];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int c = 32 * kb + 8 * (r >> 2) + (r & 3);
+        float e = fast_exp2(fmaf(logistic_of(s[r], sc), sc.a, less));
+        if (c >= over || c < under) e = 0.0f;
+        l_run += e;
+        pb[r >> 3][r & 7] = static_cast<__bf16>(e);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          const bf16x4 lo = lds_read_tr(vl + v_lane[db] + 16 * t * VSTR);
+          const bf16x4 hi = lds_read_tr(vl + v_lane[db] + (16 * t + 8) * VSTR);
+          const bf16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[t], oacc[db], 0, 0, 0);
+        }
+    }
+  };
+
   const int t_begin = it.kv_begin / KT;
   const int t_end = (it.kv_end + KT - 1) / KT;
   int pg_nxt = 0;
@@ -362,11 +479,25 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
       pg_nxt = page_of(tile + 2);
     }
     const int kbase = tile * KT;
-    if (wave_active && kbase < wave_end && (PLAIN || kbase + KT > wave_first)) {
-      // S^T[key][row] for the KT keys of the tile, as NKB 32-key blocks
+    const bool active = wave_active && kbase < wave_end && (F == CAUSAL || kbase + KT > wave_first);
+    const bool need_mask = kbase + KT > all_end || kbase + KT > it.kv_end || (F != CAUSAL && kbase < all_first);
+    const int over = min(end, it.kv_end) - kbase - 4 * hf, under = begin - kbase - 4 * hf;
+    if (F == CAPPED && active) {
+      if (need_mask) capped_edge(buf, over, under);
+      else capped_tile(buf);
+    } else if (active) {
+      // S^T[key][row] for the KT keys of the tile, as NKB 32-key blocks; accumulator element r of block kb holds key
+      // 32*kb + 8*(r/4) + 4*hf + (r%4).  A slope without a cap is what the products are added to.
       f32x16 sacc[NKB];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb) sacc[kb] = f32x16{};
+      const float from = float(rm.prefix + tok - kbase - 4 * hf);
+      if (F == LINEAR && sc.sloped) {
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sacc[kb][r] = -sc.slope * fabsf(from - float(32 * kb + 8 * (r >> 2) + (r & 3)));
+      }
       const __bf16* kl = &ks[buf][k_lane];
 #pragma unroll
       for (int s = 0; s < D / 16; ++s)
@@ -383,37 +514,22 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-      // accumulator element r of block kb holds key 32*kb + 8*(r/4) + 4*hf + (r%4)
-      if (!PLAIN) {
-        if (sc.capped) {
+      if (F == MIXED) {
 #pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
+        for (int kb = 0; kb < NKB; ++kb) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[kb][r] = sc.out * tanh_of(sacc[kb][r] * sc.in, sc.wide);
-        } else {
-#pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) sacc[kb][r] *= sl2;
-        }
-        if (sc.sloped) {
-          const float from = float(rm.prefix + tok - kbase - 4 * hf);
-#pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              sacc[kb][r] = fmaf(-sc.slope, fabsf(from - float(32 * kb + 8 * (r >> 2) + (r & 3))), sacc[kb][r]);
+          for (int r = 0; r < 16; ++r)
+            sacc[kb][r] = fmaf(-sc.slope, fabsf(from - float(32 * kb + 8 * (r >> 2) + (r & 3))), capped_of(sacc[kb][r], sc));
+          __builtin_amdgcn_sched_barrier(0);       // block by block: fewer registers
         }
       }
-      const bool need_mask = kbase + KT > all_end || kbase + KT > it.kv_end || (!PLAIN && kbase < all_first);
       if (need_mask) {
-        const int over = min(end, it.kv_end) - kbase - 4 * hf, under = begin - kbase - 4 * hf;
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int c = 32 * kb + 8 * (r >> 2) + (r & 3);
-            if (c >= over || (!PLAIN && c < under)) sacc[kb][r] = -INFINITY;
+            if (c >= over || (F != CAUSAL && c < under)) sacc[kb][r] = -INFINITY;
           }
       }
       float mx = -INFINITY;
@@ -421,21 +537,21 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
       for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[kb][r]);
-      mx = halves_max(mx);
-      if (PLAIN) mx *= sl2;
+      mx = fmaf(halves_max(mx), sc.a, sc.b);
       // The reference max only moves when the tile's max exceeds it by more than 2^8, so most tiles
       // skip rescaling the accumulators; probabilities stay below 256, which bf16/fp32 represent as
       // well as values below 1.  The final normalization uses the same reference.
       const bool bump = mx > m_run + 8.0f;
       const float m_new = bump ? mx : m_run;
       const float m_use = reference(m_new);
+      const float less = sc.b - m_use;
       float rs = 0.0f;
       bf16x8 pb[2 * NKB];
 #pragma unroll
       for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float e = fast_exp2(PLAIN ? fmaf(sacc[kb][r], sl2, -m_use) : sacc[kb][r] - m_use);
+          const float e = fast_exp2(fmaf(sacc[kb][r], sc.a, less));
           rs += e;
           pb[2 * kb + (r >> 3)][r & 7] = static_cast<__bf16>(e);
         }
@@ -476,6 +592,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   }
 
   // ---- epilogue: O = O^T / l, lse = ln(l) + m (natural log) ------------------------------------
+  if (F == CAPPED) l_run = halves_sum(l_run);
   if (!row_ok) return;
   const float sum = row_sum(m_run, l_run);
   const float inv_l = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -532,7 +649,7 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return halves_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
 }
 
-template <int D, int RT, bool PLAIN>
+template <int D, int RT, Form F>
 __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x, const __bf16* __restrict__ q,
                                                              const uint8_t* __restrict__ kpool,
                                                              const uint8_t* __restrict__ vpool, __bf16* __restrict__ out,
@@ -545,10 +662,10 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * VBYTES > JOIN ? 4 * VBYTES : JOIN];
   __shared__ float wave_m[4][16 * RT], wave_l[4][16 * RT];
 
-  if (!meta_ok(p)) return;
+  // the header, the item and its request in one trip to memory
   const WorkItem it = p.items[blockIdx.x];
-  if (it.rows <= 0) return;
-  const ReqMeta rm = p.reqs[it.req];
+  const ReqMeta rm = x.item_reqs[blockIdx.x];
+  if (int(!meta_ok(p)) | int(it.rows <= 0) | int(rm.chunk <= 0)) return;
   const int Hq = p.num_q_heads, Hkv = p.num_kv_heads;
   const int G = Hq / Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -562,7 +679,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
 
   int begin[RT], end[RT], pos[RT];               // keys that this lane's rows see, the rows' positions
   bf16x8 qf[RT][D / 32];
-  RowScores sc[RT];
+  Scores sc[RT];
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     const int lrow = 16 * t + col;
@@ -572,23 +689,20 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     pos[t] = rm.prefix + tok;
     begin[t] = 0;
     end[t] = pos[t] + 1;
-    if (!PLAIN) {
-      if (x.ranges) {
-        const TokenRange seen = x.ranges[rm.cu + tok];
-        begin[t] = seen.begin;
-        end[t] = seen.end;
-      }
-      sc[t] = row_scores(p, x, head);
+    if (F != CAUSAL && x.ranges) {
+      const TokenRange seen = x.ranges[rm.cu + tok];
+      begin[t] = seen.begin;
+      end[t] = seen.end;
     }
+    sc[t] = scores_of<F>(p, x, head);
     const __bf16* qrow = q + (int64_t(rm.cu + tok) * Hq + head) * D;
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
       qf[t][s] = row_ok ? *reinterpret_cast<const bf16x8*>(qrow + 16 * (4 * (s >> 1) + g) + 8 * (s & 1)) : bf16x8{};
   }
   // all rows see all keys from all_first to before all_end
-  const int all_first = !PLAIN && x.ranges ? INT32_MAX : 0;
-  const int all_end = !PLAIN && x.ranges ? 0 : rm.prefix + it.row0 / G + 1;
-  const float sl2 = p.softmax_scale * kLog2e;
+  const int all_first = F != CAUSAL && x.ranges ? INT32_MAX : 0;
+  const int all_end = F != CAUSAL && x.ranges ? 0 : rm.prefix + it.row0 / G + 1;
 
   struct Block {                                 // 32 keys
     u32x4 k[2][NK], v[NV];
@@ -657,42 +771,43 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     float alpha[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
-      if (!PLAIN) {
+      if (F != CAUSAL) {
         const float from = float(pos[t] - kbase - 4 * g);
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float v = s[t][kt][r];
-            v = sc[t].capped ? sc[t].out * tanh_of(v * sc[t].in, sc[t].wide) : v * sl2;
-            s[t][kt][r] = sc[t].sloped ? fmaf(-sc[t].slope, fabsf(from - float(16 * kt + r)), v) : v;
+            if (F == CAPPED) v = logistic_of(v, sc[t]);
+            if (F == MIXED) v = capped_of(v, sc[t]);
+            s[t][kt][r] = F != CAPPED && sc[t].sloped ? fmaf(-sc[t].slope, fabsf(from - float(16 * kt + r)), v) : v;
           }
       }
-      if (kbase + 32 > all_end || kbase + 32 > it.kv_end || (!PLAIN && kbase < all_first)) {
+      if (kbase + 32 > all_end || kbase + 32 > it.kv_end || (F != CAUSAL && kbase < all_first)) {
         const int over = min(end[t], it.kv_end) - kbase - 4 * g, under = begin[t] - kbase - 4 * g;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int r = 0; r < 4; ++r)
-            if (16 * kt + r >= over || (!PLAIN && 16 * kt + r < under)) s[t][kt][r] = -INFINITY;
+            if (16 * kt + r >= over || (F != CAUSAL && 16 * kt + r < under)) s[t][kt][r] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[t][kt][r]);
-      mx = quarters_max(mx);
-      if (PLAIN) mx *= sl2;
+      mx = fmaf(quarters_max(mx), sc[t].a, sc[t].b);
       bump[t] = mx > m_run[t] + 8.0f;            // as in the kernel above
       const float m_new = bump[t] ? mx : m_run[t];
       const float m_use = reference(m_new);
       alpha[t] = fast_exp2(m_run[t] - m_use);
+      const float less = sc[t].b - m_use;
       float rs = 0.0f;
 #pragma unroll
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float e = fast_exp2(PLAIN ? fmaf(s[t][kt][r], sl2, -m_use) : s[t][kt][r] - m_use);
+          const float e = fast_exp2(fmaf(s[t][kt][r], sc[t].a, less));
           rs += e;
           pb[t][4 * kt + r] = static_cast<__bf16>(e);
         }
@@ -861,27 +976,37 @@ hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few
   auto oo = static_cast<__bf16*>(out);
   const int32_t num_many = p.num_items - num_few;
   const bool w8 = p.rows_per_item == kGqaRowsPerItem, one = x.few_rows <= 16;
-  const bool plain = !x.ranges && !x.slopes && x.cap == 0.0f;
+  const Form form = x.cap > 0.0f ? (x.cap <= kFixedCap && !x.slopes ? CAPPED : MIXED) : x.ranges || x.slopes ? LINEAR : CAUSAL;
   if (num_many && !w8 && p.rows_per_item != kGqaRowsPerItem / 2) return hipErrorInvalidValue;
   DevPlan few = p;
+  Q8Dev xf = x;
   few.items += num_many;
-#define WAVEPP_Q8(D_, PLAIN_)                                                                                          \
+  xf.item_reqs += num_many;
+#define WAVEPP_Q8(D_, F_)                                                                                          \
   if (num_many && w8)                                                                                                  \
-    hipLaunchKernelGGL((attn_q8_kernel<D_, 8, PLAIN_>), dim3(num_many), dim3(512), 0, stream, p, x, qq, kp, vp, oo, lse);  \
+    hipLaunchKernelGGL((attn_q8_kernel<D_, 8, F_>), dim3(num_many), dim3(512), 0, stream, p, x, qq, kp, vp, oo, lse);  \
   else if (num_many)                                                                                                   \
-    hipLaunchKernelGGL((attn_q8_kernel<D_, 4, PLAIN_>), dim3(num_many), dim3(256), 0, stream, p, x, qq, kp, vp, oo, lse);  \
+    hipLaunchKernelGGL((attn_q8_kernel<D_, 4, F_>), dim3(num_many), dim3(256), 0, stream, p, x, qq, kp, vp, oo, lse);  \
   if (num_few && one)                                                                                                  \
-    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 1, PLAIN_>), dim3(num_few), dim3(256), 0, stream, few, x, qq, kp, vp, oo, lse); \
+    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 1, F_>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, lse); \
   else if (num_few)                                                                                                    \
-    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 2, PLAIN_>), dim3(num_few), dim3(256), 0, stream, few, x, qq, kp, vp, oo, lse);
-  if (p.head_dim_qk == 128 && plain) {
-    WAVEPP_Q8(128, true)
+    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 2, F_>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, lse);
+  if (p.head_dim_qk == 128 && form == CAUSAL) {
+    WAVEPP_Q8(128, CAUSAL)
+  } else if (p.head_dim_qk == 128 && form == LINEAR) {
+    WAVEPP_Q8(128, LINEAR)
+  } else if (p.head_dim_qk == 128 && form == CAPPED) {
+    WAVEPP_Q8(128, CAPPED)
   } else if (p.head_dim_qk == 128) {
-    WAVEPP_Q8(128, false)
-  } else if (p.head_dim_qk == 64 && plain) {
-    WAVEPP_Q8(64, true)
+    WAVEPP_Q8(128, MIXED)
+  } else if (p.head_dim_qk == 64 && form == CAUSAL) {
+    WAVEPP_Q8(64, CAUSAL)
+  } else if (p.head_dim_qk == 64 && form == LINEAR) {
+    WAVEPP_Q8(64, LINEAR)
+  } else if (p.head_dim_qk == 64 && form == CAPPED) {
+    WAVEPP_Q8(64, CAPPED)
   } else if (p.head_dim_qk == 64) {
-    WAVEPP_Q8(64, false)
+    WAVEPP_Q8(64, MIXED)
   } else {
     return hipErrorInvalidValue;
   }

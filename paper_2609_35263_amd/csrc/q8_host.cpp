@@ -33,6 +33,7 @@ Q8Dev make_q8(const wavepp_plan* plan, void* ws) {
   auto* base = static_cast<unsigned char*>(ws);
   Q8Dev x{};
   x.blocks = reinterpret_cast<const Q8Block*>(base + plan->off_blocks);
+  x.item_reqs = reinterpret_cast<const ReqMeta*>(base + plan->off_item_reqs);
   x.num_blocks = plan->num_blocks;
   x.few_rows = plan->few_rows;
   if (plan->off_ranges) x.ranges = reinterpret_cast<const TokenRange*>(base + plan->off_ranges);

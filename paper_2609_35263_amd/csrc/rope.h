@@ -10,7 +10,6 @@ constexpr int kRopeMaxPairs = 128;
 
 // A launch's arguments beside the DevPlan.
 struct RopeDev {
-  double turns[kRopeMaxPairs];       // of every pair, for one token
   int32_t pairs, offset, interleaved;
   float magnitude;
   const int32_t* positions;          // NULL: the plan's
@@ -19,6 +18,7 @@ struct RopeDev {
   int64_t q_stride, k_stride, q_out_stride, k_out_stride;
 };
 
-hipError_t launch_rope(const DevPlan& p, const RopeDev& x, hipStream_t stream);
+// turns: of every pair, for one token.
+hipError_t launch_rope(const DevPlan& p, const RopeDev& x, const double* turns, hipStream_t stream);
 
 }  // namespace wavepp

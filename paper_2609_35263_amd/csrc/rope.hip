@@ -8,34 +8,39 @@
 #include "device.h"
 #include "rope.h"
 
+#include <algorithm>
+
 namespace wavepp {
 namespace {
 
 constexpr int kThreads = 256;
 
-// The request that holds packed token t, the last with cu <= t, found by whole waves: 64 of the requests at a time.
-__device__ __forceinline__ int request_of(const DevPlan& p, int64_t t) {
+// A launch's frequencies, in turns a token: as many as the arguments need, which the host copies at every launch.
+template <int MAX>
+struct Turns {
+  double of[MAX];
+};
+
+// The position of packed token t of its request, the last with cu <= t, which whole waves find 64 requests at a time: the search
+// ends with the lane that has it.  It stays within the requests whatever it reads.
+__device__ __forceinline__ int64_t position_of(const DevPlan& p, const RopeDev& x, int64_t t) {
+  if (x.positions) return x.positions[t];
   const int lane = threadIdx.x & 63;
   int lo = 0, n = p.num_requests;                    // the request is one of n from lo on
-  while (n > 1) {
-    const int step = (n + 63) / 64, r = lo + lane * step;
-    const bool before = lane * step < n && p.reqs[min(r, p.num_requests - 1)].cu <= t;
-    const int last = 63 - __clzll((long long)__ballot(before));      // lane 0's holds
+  for (;;) {
+    const int step = (n + 63) / 64, r = min(lo + lane * step, p.num_requests - 1);
+    const int cu = p.reqs[r].cu, prefix = p.reqs[r].prefix;
+    const int last = max(63 - __clzll((long long)__ballot(lane * step < n && cu <= t)), 0);      // lane 0's holds, in a plan
+    if (step == 1) return int64_t(__builtin_amdgcn_readlane(prefix, last)) + (t - __builtin_amdgcn_readlane(cu, last));
     lo += last * step;
     n = min(step, n - last * step);
   }
-  return lo;
-}
-
-__device__ __forceinline__ int64_t position_of(const DevPlan& p, const RopeDev& x, int64_t t) {
-  if (x.positions) return x.positions[t];
-  const int r = request_of(p, t);
-  return int64_t(p.reqs[r].prefix) + (t - p.reqs[r].cu);
 }
 
 // cos and sin, times the magnitude, of pair i at a position.
-__device__ __forceinline__ float2 turn(const RopeDev& x, int64_t position, int i) {
-  const double turns = double(position) * x.turns[i];
+template <int MAX>
+__device__ __forceinline__ float2 turn(const RopeDev& x, const Turns<MAX>& f, int64_t position, int i) {
+  const double turns = double(position) * f.of[i];
   float s, c;
   sincospif(2.0f * float(turns - rint(turns)), &s, &c);
   return {c * x.magnitude, s * x.magnitude};
@@ -62,10 +67,9 @@ __device__ __forceinline__ Head head_of(const RopeDev& x, int64_t t, int h, int 
 // ---------------------------------------------------------------------------------------------
 constexpr int kUnroll = 4;
 
-template <bool PAIRS>
-__global__ __launch_bounds__(kThreads) void rope_kernel(DevPlan p, RopeDev x, int heads, int units, int turned) {
-  if (!meta_ok(p)) return;
-  __shared__ __attribute__((aligned(16))) float cs[2][kRopeMaxPairs];
+template <bool PAIRS, int MAX>
+__global__ __launch_bounds__(kThreads, 8) void rope_kernel(DevPlan p, RopeDev x, Turns<MAX> f, int heads, int units, int turned) {
+  __shared__ __attribute__((aligned(16))) float cs[2][MAX];
   const int64_t t = blockIdx.x;
   const int D = p.head_dim_qk, Hq = x.q ? p.num_q_heads : 0, H = Hq + (x.k ? p.num_kv_heads : 0);
   const int unit = threadIdx.x % units, step = kThreads / units;
@@ -93,8 +97,9 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(DevPlan p, RopeDev x, in
     }
   }
   const int64_t position = position_of(p, x, t);
+  if (!meta_ok(p)) return;                       // after the loads, not before them
   for (int i = threadIdx.x; i < x.pairs; i += kThreads) {
-    const float2 v = turn(x, position, i);
+    const float2 v = turn(x, f, position, i);
     cs[0][i] = v.x;
     cs[1][i] = v.y;
   }
@@ -143,14 +148,14 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(DevPlan p, RopeDev x, in
 }
 
 // Pairs that do not come in whole 16-byte pieces: value by value, a workgroup a token.
-__global__ __launch_bounds__(kThreads) void rope_any_kernel(DevPlan p, RopeDev x, int copy_q, int copy_k) {
+__global__ __launch_bounds__(kThreads) void rope_any_kernel(DevPlan p, RopeDev x, Turns<kRopeMaxPairs> f, int copy_q, int copy_k) {
   if (!meta_ok(p)) return;
   __shared__ float cs[2][kRopeMaxPairs];
   const int64_t t = blockIdx.x;
   const int D = p.head_dim_qk, Hq = x.q ? p.num_q_heads : 0, H = Hq + (x.k ? p.num_kv_heads : 0);
   const int64_t position = position_of(p, x, t);
   for (int i = threadIdx.x; i < x.pairs; i += kThreads) {
-    const float2 v = turn(x, position, i);
+    const float2 v = turn(x, f, position, i);
     cs[0][i] = v.x;
     cs[1][i] = v.y;
   }
@@ -174,12 +179,22 @@ __global__ __launch_bounds__(kThreads) void rope_any_kernel(DevPlan p, RopeDev x
 
 }  // namespace
 
-hipError_t launch_rope(const DevPlan& p, const RopeDev& x, hipStream_t stream) {
+namespace {
+template <int MAX>
+Turns<MAX> turns_of(const double* turns, int pairs) {
+  Turns<MAX> f{};
+  std::copy(turns, turns + pairs, f.of);
+  return f;
+}
+}  // namespace
+
+hipError_t launch_rope(const DevPlan& p, const RopeDev& x, const double* turns, hipStream_t stream) {
   if (p.total_tokens >= 1 << 30) return hipErrorInvalidValue;
   const int D = p.head_dim_qk, H = (x.q ? p.num_q_heads : 0) + (x.k ? p.num_kv_heads : 0);
   const int copy_q = x.q != x.q_out, copy_k = x.k != x.k_out;
   if (x.offset % 8 || (x.interleaved ? x.pairs % 4 : x.pairs % 8)) {
-    hipLaunchKernelGGL(rope_any_kernel, dim3(unsigned(p.total_tokens)), dim3(kThreads), 0, stream, p, x, copy_q, copy_k);
+    hipLaunchKernelGGL(rope_any_kernel, dim3(unsigned(p.total_tokens)), dim3(kThreads), 0, stream, p, x,
+                       turns_of<kRopeMaxPairs>(turns, x.pairs), copy_q, copy_k);
     return hipGetLastError();
   }
   const int turned = x.interleaved ? x.pairs / 4 : x.pairs / 8;
@@ -188,10 +203,17 @@ hipError_t launch_rope(const DevPlan& p, const RopeDev& x, hipStream_t stream) {
   const int most = kThreads / units * kUnroll, parts = (H + most - 1) / most, heads = (H + parts - 1) / parts;
   if (parts > 65535) return hipErrorInvalidValue;
   const dim3 grid(unsigned(p.total_tokens), unsigned(parts));
-  if (x.interleaved)
-    hipLaunchKernelGGL((rope_kernel<true>), grid, dim3(kThreads), 0, stream, p, x, heads, units, turned);
-  else
-    hipLaunchKernelGGL((rope_kernel<false>), grid, dim3(kThreads), 0, stream, p, x, heads, units, turned);
+#define WAVEPP_ROPE(PAIRS_, MAX_)                                                                                      \
+  hipLaunchKernelGGL((rope_kernel<PAIRS_, MAX_>), grid, dim3(kThreads), 0, stream, p, x, turns_of<MAX_>(turns, x.pairs), \
+                     heads, units, turned)
+  if (x.pairs <= 32) {
+    if (x.interleaved) WAVEPP_ROPE(true, 32); else WAVEPP_ROPE(false, 32);
+  } else if (x.pairs <= 64) {
+    if (x.interleaved) WAVEPP_ROPE(true, 64); else WAVEPP_ROPE(false, 64);
+  } else {
+    if (x.interleaved) WAVEPP_ROPE(true, kRopeMaxPairs); else WAVEPP_ROPE(false, kRopeMaxPairs);
+  }
+#undef WAVEPP_ROPE
   return hipGetLastError();
 }
 

@@ -14,7 +14,8 @@ using namespace wavepp;
 struct wavepp_rope {
   int32_t pairs = 0, offset = 0, interleaved = 0;
   float magnitude = 1.0f;
-  double frequencies[kRopeMaxPairs] = {};
+  double frequencies[kRopeMaxPairs] = {}, turns[kRopeMaxPairs] = {};
+  void take_turns();
 };
 
 namespace {
@@ -43,6 +44,10 @@ bool positive(double x) { return x > 0.0 && std::isfinite(x); }
 
 }  // namespace
 
+void wavepp_rope::take_turns() {
+  for (int32_t i = 0; i < pairs; ++i) turns[i] = frequencies[i] / kTurn;
+}
+
 extern "C" {
 
 int wavepp_rope_create(const wavepp_rope_spec* spec, wavepp_rope** out) {
@@ -67,6 +72,7 @@ int wavepp_rope_create(const wavepp_rope_spec* spec, wavepp_rope** out) {
       if (!std::isfinite(s.frequencies[i])) return set_error(WAVEPP_EINVAL, "frequency %d is not finite", i);
       rope->frequencies[i] = s.frequencies[i];
     }
+    rope->take_turns();
     *out = rope.release();
     return WAVEPP_OK;
   }
@@ -95,6 +101,7 @@ int wavepp_rope_create(const wavepp_rope_spec* spec, wavepp_rope** out) {
     rope->frequencies[i] = w == 1.0 ? f : w * f + (1.0 - w) * f / s.factor;
     if (!std::isfinite(rope->frequencies[i])) return set_error(WAVEPP_EINVAL, "frequency %d is not finite", i);
   }
+  rope->take_turns();
   *out = rope.release();
   return WAVEPP_OK;
 }
@@ -151,7 +158,6 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
       if (rows_meet(reinterpret_cast<uintptr_t>(positions), 4, 4, rows[o].at, rows[o].stride, rows[o].width, T))
         return set_error(WAVEPP_EALIAS, "%s and positions overlap", rows[o].name);
   RopeDev x{};
-  for (int32_t i = 0; i < rope->pairs; ++i) x.turns[i] = rope->frequencies[i] / kTurn;
   x.pairs = rope->pairs;
   x.offset = rope->offset;
   x.interleaved = rope->interleaved;
@@ -165,7 +171,7 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
   x.k_stride = k_stride;
   x.q_out_stride = q_out_stride;
   x.k_out_stride = k_out_stride;
-  const hipError_t e = launch_rope(make_dev(plan, workspace), x, stream);
+  const hipError_t e = launch_rope(make_dev(plan, workspace), x, rope->turns, stream);
   return e == hipSuccess ? WAVEPP_OK : set_hip_error(e, "rope launch");
 }
 

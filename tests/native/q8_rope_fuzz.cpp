@@ -19,7 +19,7 @@ hipError_t launch_q8_read(const DevPlan&, const Q8Dev&, const void*, const void*
 hipError_t launch_q8_attention(const DevPlan&, const Q8Dev&, int32_t, const void*, const void*, const void*, void*, float*, hipStream_t) {
   return hipErrorNotSupported;
 }
-hipError_t launch_rope(const DevPlan&, const RopeDev&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rope(const DevPlan&, const RopeDev&, const double*, hipStream_t) { return hipErrorNotSupported; }
 }  // namespace wavepp
 
 static long left = -1;                               // allocations until the one that fails; < 0: none does
