@@ -62,7 +62,8 @@ size_t wavepp_q8_page_bytes(int32_t head_dim, int32_t page_size);
 
 /* wavepp_attn_plan for an 8-bit cache.  Supported: (head_dim_qk, head_dim_v) in {(64, 64), (128, 128)}, kv_shared = 0, any
  * num_q_heads % num_kv_heads == 0, page_size in {16, 64}; a latent cache is WAVEPP_EUNSUPPORTED.  scores may be NULL; one
- * out of the ranges above is WAVEPP_EINVAL.  Arguments and errors otherwise as there. */
+ * out of the ranges above is WAVEPP_EINVAL, as is a softmax_scale over 1e30 times a cap or under 1e-20 beside slopes.
+ * Arguments and errors otherwise as there. */
 int wavepp_q8_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, const wavepp_q8_scores* scores,
                    int32_t max_splits, wavepp_plan** out);
 
@@ -86,7 +87,8 @@ int wavepp_q8_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
  * softmax.  A row whose softmax sum is not a number (a NaN in its query, a largest score that overflows or lies beyond
  * 2^28 ln 2, where fp32 cannot place its exponential) has NaN as its output and its lse, whole or joined from splits.
  * Scores under -2^28 ln 2 have no weight; an lse of -infinity says that no key had any, and the output is then zero.  A
- * capped score is off by at most 2^-20 of itself plus, for a cap of 128 or less, 2^-21 of the cap.
+ * capped score is off by at most 2^-20 of itself plus, for a cap of 128 or less, 2^-21 of the cap.  With a cap of 50 or
+ * less and no slopes, weights of up to 2^65 are summed, so values of V over 2^40 may overflow to infinity.
  * Deterministic: repeated calls give bit-identical results.  Errors as for wavepp_attn_chunked_prefill. */
 int wavepp_q8_chunked_prefill(const wavepp_plan* plan, const void* q, const void* k_pool, const void* v_pool, void* out,
                               float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);

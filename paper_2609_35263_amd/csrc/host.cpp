@@ -750,6 +750,11 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       return set_error(WAVEPP_EINVAL, "the scores' cap must be finite and not negative");
     if (scores->cap > 0.0f && !(scores->cap >= 1e-3f && scores->cap <= 1e6f))
       return set_error(WAVEPP_EINVAL, "the scores' cap must lie in [1e-3, 1e6], or be 0 for none");
+    // what the kernels multiply products by, and divide slopes by, has to be a number of fp32's middle range
+    if (scores->cap > 0.0f && !(s.softmax_scale <= 1e30f * std::min(scores->cap, 1.0f)))
+      return set_error(WAVEPP_EINVAL, "softmax_scale must be at most 1e30 times the cap");
+    if (scores->slopes && !(s.softmax_scale >= 1e-20f))
+      return set_error(WAVEPP_EINVAL, "softmax_scale must be at least 1e-20 with slopes");
     if (scores->slopes)
       for (int32_t h = 0; h < s.num_q_heads; ++h)
         if (!(std::fabs(scores->slopes[h]) <= 1024.0f))

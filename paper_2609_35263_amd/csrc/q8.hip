@@ -43,19 +43,21 @@ __device__ __forceinline__ u32x2 q8_codes(u32x4 y, float s) {
   return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
 }
 
-// Largest value of the wave, on all lanes: within 16 lanes by lane moves, the four rows by the scalar unit.
-template <int CTRL>
-__device__ __forceinline__ uint32_t max_moved(uint32_t x) {
-  return max(x, uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, true)));
+// The wave's largest value (MAX) or smallest, on all lanes: within 16 lanes by lane moves, the four rows by the scalar unit.
+template <bool MAX, int CTRL, typename T>
+__device__ __forceinline__ T more_moved(T x) {
+  const T y = T(__builtin_amdgcn_update_dpp(0, int(x), CTRL, 0xF, 0xF, true));
+  return MAX ? max(x, y) : min(x, y);
 }
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-  x = max_moved<0xB1>(x);                    // lanes 1, 0, 3, 2 of each four
-  x = max_moved<0x4E>(x);                    // lanes 2, 3, 0, 1
-  x = max_moved<0x141>(x);                   // the other four of each eight, mirrored
-  x = max_moved<0x140>(x);                   // the other eight of each row of 16, mirrored
-  const uint32_t a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16);
-  const uint32_t c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
-  return max(max(a, b), max(c, d));
+template <bool MAX, typename T>
+__device__ __forceinline__ T wave_most(T x) {
+  x = more_moved<MAX, 0xB1>(x);              // lanes 1, 0, 3, 2 of each four
+  x = more_moved<MAX, 0x4E>(x);              // lanes 2, 3, 0, 1
+  x = more_moved<MAX, 0x141>(x);             // the other four of each eight, mirrored
+  x = more_moved<MAX, 0x140>(x);             // the other eight of each row of 16, mirrored
+  const T a = T(__builtin_amdgcn_readlane(x, 0)), b = T(__builtin_amdgcn_readlane(x, 16));
+  const T c = T(__builtin_amdgcn_readlane(x, 32)), d = T(__builtin_amdgcn_readlane(x, 48));
+  return MAX ? max(max(a, b), max(c, d)) : min(min(a, b), min(c, d));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(256) void q8_append_kernel(DevPlan p, Q8Dev x, cons
       v[i][w] = (v[i][w] & 0x80008000u) | lo | (hi << 16);
       top = max(top, max(lo, hi));
     }
-  top = wave_max(top);
+  top = wave_most<true>(top);
   // top = 1.m * 2^(E - 127): the smallest s with top <= 1.75 * 2^8 s is 2^(E - 127 - 8), twice that where 1.m > 1.75
   const int e = max(max(int(top >> 7) - 8 + int((top & 0x7Fu) > 0x60u), 8), e_held);
   const float s = scale_of(uint32_t(e));
@@ -178,8 +180,9 @@ __device__ __forceinline__ float row_sum(float m, float l) { return m <= kFarSco
 enum Form { CAUSAL, LINEAR, CAPPED, MIXED };
 
 // Scores of CAPPED lie within c = cap log2 e of 0, so their weights need no running reference: they are taken against one fixed
-// at min(c, 80 - c), which leaves them within 2^-80 and 2^(2 c - 80), sums and products with values up to 2^40 far inside fp32.
-constexpr float kFixedCap = 55.0f;
+// at min(c, 80 - c).  That leaves them within 2^-80 and 2^(2 c - 80), 2^65 at most: sums over 2^20 keys and their products with
+// values within 2^-40 and 2^40 stay well inside fp32.
+constexpr float kFixedCap = 50.0f;
 
 // One lane's query row's scores.  A product's accumulator becomes a value x whose score is a x + b, so the weight is one fused
 // multiply-add and one exp2 of x in every form:
@@ -269,6 +272,31 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   const uint8_t* __restrict__ kpool_h = kpool + it.kv_head * page_bytes;
   const uint8_t* __restrict__ vpool_h = vpool + it.kv_head * page_bytes;
 
+  // ---- K/V tile staging -----------------------------------------------------------------------
+  // Thread tid has a quarter of key tid / 4's row.  Positions past the request's last valid one are clamped to that
+  // one: finite copies that the mask gives zero weight, so stale slots are never read.
+  const int key = tid >> 2, part = tid & 3;
+  u32x4 kreg[W], vreg[W];
+  uint32_t kscale = 0, vscale = 0;
+  // The page of this wave's keys is looked up one tile ahead.
+  auto page_of = [&](int tile) { return const_load(bt + (min(tile * KT + wave * 16, last) >> shift)); };
+  auto load_tile = [&](int tile, int page) {
+    const int j = min(tile * KT + key, last), j0 = min(tile * KT + wave * 16, last);
+    const int64_t at = int64_t(page) * page_stride;
+    const uint32_t off = uint32_t(j & (B - 1)) * D + part * (W * 16);
+    const uint32_t soff = uint32_t(B * D) + uint32_t((j0 & (B - 1)) >> 4);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      kreg[i] = *reinterpret_cast<const u32x4*>(kpool_h + at + off + 16 * i);
+      vreg[i] = *reinterpret_cast<const u32x4*>(vpool_h + at + off + 16 * i);
+    }
+    kscale = (kpool_h + at)[soff];
+    vscale = (vpool_h + at)[soff];
+  };
+  const int t_begin = it.kv_begin / KT;
+  const int t_end = (it.kv_end + KT - 1) / KT;
+  if (t_begin < t_end) load_tile(t_begin, page_of(t_begin));       // under way while the rows are looked up
+
   // ---- this lane's query row -----------------------------------------------------------------
   const int lrow = wave * 32 + col;
   const bool row_ok = lrow < it.rows;
@@ -300,17 +328,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
       wave_end = row_ok && begin < end ? end : 0;
       all_first = row_ok ? begin : 0;
       all_end = row_ok ? end : INT32_MAX;
-#pragma unroll
-      for (int m = 1; m < 32; m <<= 1) {
-        wave_first = min(wave_first, __shfl_xor(wave_first, m));
-        wave_end = max(wave_end, __shfl_xor(wave_end, m));
-        all_first = max(all_first, __shfl_xor(all_first, m));
-        all_end = min(all_end, __shfl_xor(all_end, m));
-      }
-      wave_first = __builtin_amdgcn_readfirstlane(wave_first);
-      wave_end = __builtin_amdgcn_readfirstlane(wave_end);
-      all_first = __builtin_amdgcn_readfirstlane(all_first);
-      all_end = __builtin_amdgcn_readfirstlane(all_end);
+      wave_first = wave_most<false>(wave_first);
+      wave_end = wave_most<true>(wave_end);
+      all_first = wave_most<true>(all_first);
+      all_end = wave_most<false>(all_end);
     }
   }
 
@@ -319,27 +340,6 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
   float m_run = F == CAPPED ? fixed_reference(sc) : -INFINITY, l_run = 0.0f;      // CAPPED: l_run is of half of the keys
 
-  // ---- K/V tile staging -----------------------------------------------------------------------
-  // Thread tid has a quarter of key tid / 4's row.  Positions past the request's last valid one are clamped to that
-  // one: finite copies that the mask gives zero weight, so stale slots are never read.
-  const int key = tid >> 2, part = tid & 3;
-  u32x4 kreg[W], vreg[W];
-  uint32_t kscale = 0, vscale = 0;
-  // The page of this wave's keys is looked up one tile ahead.
-  auto page_of = [&](int tile) { return const_load(bt + (min(tile * KT + wave * 16, last) >> shift)); };
-  auto load_tile = [&](int tile, int page) {
-    const int j = min(tile * KT + key, last), j0 = min(tile * KT + wave * 16, last);
-    const int64_t at = int64_t(page) * page_stride;
-    const uint32_t off = uint32_t(j & (B - 1)) * D + part * (W * 16);
-    const uint32_t soff = uint32_t(B * D) + uint32_t((j0 & (B - 1)) >> 4);
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      kreg[i] = *reinterpret_cast<const u32x4*>(kpool_h + at + off + 16 * i);
-      vreg[i] = *reinterpret_cast<const u32x4*>(vpool_h + at + off + 16 * i);
-    }
-    kscale = (kpool_h + at)[soff];
-    vscale = (vpool_h + at)[soff];
-  };
   auto store_tile = [&](int buf) {
     __bf16* kd = &ks[buf][key * KSTR + part * (W * 16)];
     const float a = scale_of(kscale), b = scale_of(vscale);
@@ -461,11 +461,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
     }
   };
 
-  const int t_begin = it.kv_begin / KT;
-  const int t_end = (it.kv_end + KT - 1) / KT;
   int pg_nxt = 0;
   if (t_begin < t_end) {
-    load_tile(t_begin, page_of(t_begin));
     store_tile(0);
     pg_nxt = page_of(t_begin + 1);
   }
@@ -480,10 +477,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
     }
     const int kbase = tile * KT;
     const bool active = wave_active && kbase < wave_end && (F == CAUSAL || kbase + KT > wave_first);
-    const bool need_mask = kbase + KT > all_end || kbase + KT > it.kv_end || (F != CAUSAL && kbase < all_first);
+    const bool mask_over = kbase + KT > all_end || kbase + KT > it.kv_end, mask_under = F != CAUSAL && kbase < all_first;
     const int over = min(end, it.kv_end) - kbase - 4 * hf, under = begin - kbase - 4 * hf;
     if (F == CAPPED && active) {
-      if (need_mask) capped_edge(buf, over, under);
+      if (mask_over || mask_under) capped_edge(buf, over, under);
       else capped_tile(buf);
     } else if (active) {
       // S^T[key][row] for the KT keys of the tile, as NKB 32-key blocks; accumulator element r of block kb holds key
@@ -523,14 +520,19 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
           __builtin_amdgcn_sched_barrier(0);       // block by block: fewer registers
         }
       }
-      if (need_mask) {
+      if (mask_over) {
 #pragma unroll
         for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int c = 32 * kb + 8 * (r >> 2) + (r & 3);
-            if (c >= over || (F != CAUSAL && c < under)) sacc[kb][r] = -INFINITY;
-          }
+          for (int r = 0; r < 16; ++r)
+            if (32 * kb + 8 * (r >> 2) + (r & 3) >= over) sacc[kb][r] = -INFINITY;
+      }
+      if (mask_under) {
+#pragma unroll
+        for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (32 * kb + 8 * (r >> 2) + (r & 3) < under) sacc[kb][r] = -INFINITY;
       }
       float mx = -INFINITY;
 #pragma unroll
@@ -936,7 +938,7 @@ int64_t move_groups(const DevPlan& p, const Q8Dev& x) { return int64_t((x.num_bl
 hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new, const void* v_new, void* k_pool,
                             void* v_pool, hipStream_t stream) {
   const int64_t groups = move_groups(p, x);
-  if (groups >= 1 << 30) return hipErrorInvalidValue;
+  if (groups >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
   auto kn = static_cast<const u32x4*>(k_new);
   auto vn = static_cast<const u32x4*>(v_new);
   auto kp = static_cast<uint8_t*>(k_pool);
@@ -953,7 +955,7 @@ hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new,
 hipError_t launch_q8_read(const DevPlan& p, const Q8Dev& x, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                           hipStream_t stream) {
   const int64_t groups = move_groups(p, x);
-  if (groups >= 1 << 30) return hipErrorInvalidValue;
+  if (groups >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
   auto kp = static_cast<const uint8_t*>(k_pool);
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto ko = static_cast<bf16x8*>(k_out);

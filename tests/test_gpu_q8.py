@@ -257,7 +257,7 @@ def score_forms(spec, rng):
     shared = np.minimum(n, np.maximum(pos + 1, start + 15))                  # whose first 15 tokens all of one sees
     any_lo, any_hi = rng.integers(0, n + 1), rng.integers(0, n + 1)          # half of them empty
     return {
-        "cap": {"cap": 2.0}, "wide_cap": {"cap": 500.0}, "slopes": {"slopes": slopes},
+        "cap": {"cap": 2.0}, "largest_fixed_cap": {"cap": 50.0}, "cap_over_it": {"cap": 50.5}, "wide_cap": {"cap": 500.0}, "slopes": {"slopes": slopes},
         "window": {"key_begin": window}, "documents": {"key_begin": start},
         "prefix": {"key_begin": start, "key_end": shared}, "all_keys": {"key_end": n},
         "any": {"key_begin": any_lo, "key_end": any_hi}, "nothing": {"key_begin": pos + 1}, "nothing_at_all": {"key_end": pos * 0},
@@ -313,6 +313,23 @@ def test_large_and_small_logits(scale):
     t["q"] = (t["q"].float() * scale).to(torch.bfloat16)
     check(spec, t, on_gpu(spec, t), f"x {scale}")
     check(spec, t, on_gpu(spec, t, score_cap=20.0), f"x {scale}, capped", cap=20.0)
+
+
+@pytest.mark.parametrize("name", ["tokens", "few_rows_mixed", "four_waves", "eight_waves"])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_all_at_their_cap(name, sign):
+    """Every score of every row at a cap of 50, or at -50: the weights are alike, so the output is the values' mean."""
+    q, kv, dim, page, prefix, chunk = WAVES[name]
+    spec = wl.custom_wave(q, kv, dim, dim, page, prefix, chunk, seed=53, name=name)
+    t = make(spec, 54, garbage=False)
+    t["q"] = (t["q"].abs() * 1000.0 * sign).to(torch.bfloat16)
+    t["k_new"] = t["k_new"].abs() + 0.5
+    held = oracle.q8.pool_values(t["k_pool"].numpy(), dim, page)
+    t["k_pool"] = torch.from_numpy(oracle.q8.quantise_pool(np.abs(held) + 0.5))
+    for splits in (0, 3):
+        g = on_gpu(spec, t, max_splits=splits, score_cap=50.0)
+        check(spec, t, g, f"{sign} splits {splits}", cap=50.0)
+        assert (g["lse"] - 50.0 * sign >= -1e-4).all() and (g["lse"] - 50.0 * sign < 8.0).all()
 
 
 def test_stale_slots_and_later_tokens_do_not_leak():

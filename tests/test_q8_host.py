@@ -33,6 +33,7 @@ def test_plans_refuse_what_the_bf16_cache_refuses_and_latent_caches(over, status
 @pytest.mark.parametrize("scores", [
     dict(score_cap=-1.0), dict(score_cap=float("nan")), dict(score_cap=float("inf")), dict(score_cap=1e-4), dict(score_cap=2e6),
     dict(slopes=[0.0] * 7 + [float("nan")]), dict(slopes=[0.0] * 7 + [1025.0]), dict(slopes=[-float("inf")] * 8),
+    dict(score_cap=1.0, softmax_scale=2e30), dict(score_cap=1e-3, softmax_scale=2e27), dict(slopes=[0.1] * 8, softmax_scale=1e-21),
     dict(key_begin=[-1] * 32), dict(key_begin=[0] * 31 + [81]), dict(key_end=[0] * 31 + [81]), dict(key_end=[80] * 31 + [-1]),
 ])
 def test_plans_refuse_scores_out_of_range(scores):
@@ -49,7 +50,7 @@ def test_the_binding_refuses_arrays_of_another_shape_or_kind(scores):
 
 
 def test_scores_at_the_ends_of_their_ranges():
-    for s in (dict(score_cap=1e-3), dict(score_cap=1e6), dict(slopes=[1024.0, -1024.0] * 4), dict(key_begin=[0, 80] * 16, key_end=[80, 0] * 16),
+    for s in (dict(score_cap=1e-3, softmax_scale=9e26), dict(slopes=[0.1] * 8, softmax_scale=2e-20), dict(score_cap=1e-3), dict(score_cap=1e6), dict(slopes=[1024.0, -1024.0] * 4), dict(key_begin=[0, 80] * 16, key_end=[80, 0] * 16),
               dict(key_begin=[80] * 32), dict(key_end=[0] * 32)):
         assert wp.q8_plan(**kw(**s)).info()["total_tokens"] == 32
 
