@@ -405,12 +405,25 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+_is_initialized = _get_device = _current_stream = None
+
+
+def _current_device():
+    """The current device's index, -2 where nothing has used a device yet (no tensor is on one then)."""
+    global _is_initialized, _get_device, _current_stream
+    if _get_device is None:
+        import torch
+        # straight to the runtime: the checks in front of it are made here, and cost as much as the call
+        _is_initialized, _get_device = torch.cuda.is_initialized, torch._C._cuda_getDevice
+        _current_stream = torch._C._cuda_getCurrentRawStream
+    return _get_device() if _is_initialized() else -2
+
+
 def _call_args(stream, *buffers):
     """Device addresses of a call's buffers (name, tensor, shape or None for any, dtype or None for any), then the stream, for
     a call that launches on the current device: every buffer is a contiguous tensor on it of that shape and type, and so is
     the stream."""
-    import torch
-    here = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    here = _current_device()
     args = []
     for name, t, shape, dtype in buffers:
         if t is None or t.get_device() != here or (shape is not None and t.shape != shape) or \
@@ -419,7 +432,7 @@ def _call_args(stream, *buffers):
         args.append(t.data_ptr())
     if stream is None:
         # the current stream's handle alone: a Stream object costs 2.5 us, a third of such a call
-        args.append(torch._C._cuda_getCurrentRawStream(here))
+        args.append(_current_stream(here))
     elif stream.device.index != here:
         raise ValueError(f"the stream is of {stream.device}, the current device is {here}")
     else:
@@ -766,22 +779,19 @@ class Rope:
 
 def _row_args(here, name, t, shape, dtype):
     """(address, elements from token to token) of rows [T, heads, dim] whose tokens may lie apart."""
+    width = shape[1] * shape[2]
+    if t.get_device() == here and t.shape == shape and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr(), width
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, the current device is {here}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the plan needs {shape}")
     if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    width = shape[1] * shape[2]
-    if shape[0] <= 1 or t.is_contiguous():
-        step = width
-    else:
-        step = t.stride(0)
-    if step != width or not t.is_contiguous():
-        s = t.stride()
-        if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
-            raise ValueError(f"{name} must be contiguous within a token, its strides are {s}")
-    return t.data_ptr(), step
+    s = t.stride()
+    if (s[2] != 1 and shape[2] > 1) or (s[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name} must be contiguous within a token, its strides are {s}")
+    return t.data_ptr(), s[0] if shape[0] > 1 else width
 
 
 def rope_apply(rope: Rope, p: Plan, q, k, q_out, k_out, workspace, positions=None, stream=None):
@@ -790,9 +800,8 @@ def rope_apply(rope: Rope, p: Plan, q, k, q_out, k_out, workspace, positions=Non
     one packed projection."""
     if (q is None) != (q_out is None) or (k is None) != (k_out is None):
         raise ValueError("q and q_out, and k and k_out, come together")
-    import torch
-    bf = torch.bfloat16
-    here = torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    bf = _types[0] if _types else _torch_types()[0]
+    here = _current_device()
     sh = p._buffers or _attn_shapes(p)
     q_at = q_step = qo_at = qo_step = k_at = k_step = ko_at = ko_step = at = None
     if q is not None:
@@ -804,6 +813,7 @@ def rope_apply(rope: Rope, p: Plan, q, k, q_out, k_out, workspace, positions=Non
     if positions is None:
         ws, st = _call_args(stream, ("workspace", workspace, None, None))
     else:
+        import torch
         ws, at, st = _call_args(stream, ("workspace", workspace, None, None), ("positions", positions, sh["q"][:1], torch.int32))
     _check(load_library().wavepp_rope_apply(rope.handle, p.handle, q_at, q_step or 0, k_at, k_step or 0, qo_at, qo_step or 0,
                                             ko_at, ko_step or 0, at, ws, workspace.nbytes, st))
