@@ -33,6 +33,7 @@ struct wavepp_plan {
   int32_t num_real_items = 0;
   int32_t num_few = 0;                // the last items, which run with few rows over 4-bit or 8-bit pages
   int32_t few_rows = 0;               // most rows of such an item
+  bool stream = false;                // 8-bit pages: hardly a page is in two requests
   std::vector<wavepp::WorkItem> items;
   std::vector<wavepp::MergeItem> merges;      // those that merge_wide_kernel takes first
   int32_t num_merge_wide = 0, merge_rows = 0;

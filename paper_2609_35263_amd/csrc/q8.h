@@ -28,6 +28,7 @@ struct Q8Dev {
   const ReqMeta* item_reqs;    // of every work item
   int32_t num_blocks;
   int32_t few_rows;            // most rows of an item that runs with few rows
+  bool stream;                 // such items read pages that hardly another reads
   const TokenRange* ranges;    // of every new token; NULL: causal
   const float* slopes;         // of every query head; NULL: none
   float cap;                   // 0: none

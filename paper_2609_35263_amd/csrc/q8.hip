@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void q8_append_kernel(DevPlan p, Q8Dev x, cons
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
     const int row = min(max(i * RPP + first, u.lo), u.hi - 1);         // others' rows stand in for those that are not new
-    v[i] = rows[int64_t(row - u.lo) * Hkv * LPR];
+    v[i] = __builtin_nontemporal_load(rows + int64_t(row - u.lo) * Hkv * LPR);
   }
   if (u.lo > 0) {                            // the block holds earlier tokens
 #pragma unroll
@@ -641,6 +641,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
 // product in the order (g, kt, r), the probabilities are its operand where they lie.
 // ---------------------------------------------------------------------------------------------
 
+// 16 bytes, where STREAM without a place in the caches.
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load16(const uint8_t* at) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+  else return *reinterpret_cast<const u32x4*>(at);
+}
+
 // Largest value, and the sum, over the four lanes l % 16 + 16 g of a query row.
 __device__ __forceinline__ float quarters_max(float v) {
   const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -651,7 +658,7 @@ __device__ __forceinline__ float quarters_sum(float v) {
   return halves_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
 }
 
-template <int D, int RT, Form F>
+template <int D, int RT, Form F, bool STREAM>
 __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x, const __bf16* __restrict__ q,
                                                              const uint8_t* __restrict__ kpool,
                                                              const uint8_t* __restrict__ vpool, __bf16* __restrict__ out,
@@ -719,13 +726,13 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     for (int kt = 0; kt < 2; ++kt) {
       const uint32_t off = uint32_t(min(kbase + 16 * kt + col, last) & (B - 1)) * D + 16 * g;
 #pragma unroll
-      for (int i = 0; i < NK; ++i) b.k[kt][i] = *reinterpret_cast<const u32x4*>(kpool_h + at[kt] + off + 64 * i);
+      for (int i = 0; i < NK; ++i) b.k[kt][i] = load16<STREAM>(kpool_h + at[kt] + off + 64 * i);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int piece = lane + 64 * i;
       const uint32_t off = uint32_t(min(kbase + piece / PPR, last) & (B - 1)) * D + 16 * (piece % PPR);
-      b.v[i] = *reinterpret_cast<const u32x4*>(vpool_h + at[64 * i / D] + off);
+      b.v[i] = load16<STREAM>(vpool_h + at[64 * i / D] + off);
     }
     const uint8_t* pool = lane & 2 ? vpool_h : kpool_h;
     const int j = min(kbase + 16 * (lane & 1), last);
@@ -984,15 +991,23 @@ hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few
   Q8Dev xf = x;
   few.items += num_many;
   xf.item_reqs += num_many;
+#define WAVEPP_Q8_FEW(D_, RT_, F_)                                                                                     \
+  if (x.stream)                                                                                                        \
+    hipLaunchKernelGGL((attn_q8_few_kernel<D_, RT_, F_, true>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, \
+                       lse);                                                                                           \
+  else                                                                                                                 \
+    hipLaunchKernelGGL((attn_q8_few_kernel<D_, RT_, F_, false>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, \
+                       lse);
 #define WAVEPP_Q8(D_, F_)                                                                                          \
   if (num_many && w8)                                                                                                  \
     hipLaunchKernelGGL((attn_q8_kernel<D_, 8, F_>), dim3(num_many), dim3(512), 0, stream, p, x, qq, kp, vp, oo, lse);  \
   else if (num_many)                                                                                                   \
     hipLaunchKernelGGL((attn_q8_kernel<D_, 4, F_>), dim3(num_many), dim3(256), 0, stream, p, x, qq, kp, vp, oo, lse);  \
-  if (num_few && one)                                                                                                  \
-    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 1, F_>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, lse); \
-  else if (num_few)                                                                                                    \
-    hipLaunchKernelGGL((attn_q8_few_kernel<D_, 2, F_>), dim3(num_few), dim3(256), 0, stream, few, xf, qq, kp, vp, oo, lse);
+  if (num_few && one) {                                                                                                \
+    WAVEPP_Q8_FEW(D_, 1, F_)                                                                                           \
+  } else if (num_few) {                                                                                                \
+    WAVEPP_Q8_FEW(D_, 2, F_)                                                                                           \
+  }
   if (p.head_dim_qk == 128 && form == CAUSAL) {
     WAVEPP_Q8(128, CAUSAL)
   } else if (p.head_dim_qk == 128 && form == LINEAR) {
@@ -1013,6 +1028,7 @@ hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few
     return hipErrorInvalidValue;
   }
 #undef WAVEPP_Q8
+#undef WAVEPP_Q8_FEW
   return hipGetLastError();
 }
 

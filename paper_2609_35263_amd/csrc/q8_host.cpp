@@ -36,6 +36,7 @@ Q8Dev make_q8(const wavepp_plan* plan, void* ws) {
   x.item_reqs = reinterpret_cast<const ReqMeta*>(base + plan->off_item_reqs);
   x.num_blocks = plan->num_blocks;
   x.few_rows = plan->few_rows;
+  x.stream = plan->stream;
   if (plan->off_ranges) x.ranges = reinterpret_cast<const TokenRange*>(base + plan->off_ranges);
   if (plan->off_slopes) x.slopes = reinterpret_cast<const float*>(base + plan->off_slopes);
   x.cap = plan->cap;

@@ -402,10 +402,16 @@ def test_repeated_calls_and_page_orders_are_bit_identical():
     assert same(a["out"], c["out"]) and same(a["lse"], c["lse"])
 
 
-def test_shared_prefix_pages():
-    spec = wl.custom_wave(8, 2, 64, 64, 16, [64, 64, 64], [1, 2, 1], seed=22, shared_prefix_pages=3, name="shared")
+@pytest.mark.parametrize("form", [None, "cap", "slopes", "window", "mixed"])
+@pytest.mark.parametrize("q,kv,dim,page", [(8, 2, 64, 16), (32, 1, 64, 64), (16, 2, 128, 64), (40, 2, 128, 16)])
+def test_shared_prefix_pages(q, kv, dim, page, form):
+    """Requests that read the same pages (few rows are then loaded through the caches, otherwise past them)."""
+    spec = wl.custom_wave(q, kv, dim, dim, page, [192, 192, 192], [1, 1, 1], seed=22, shared_prefix_pages=192 // page, name="shared")
     t = make(spec, 23)
-    check(spec, t, on_gpu(spec, t))
+    s = {} if form is None else score_forms(spec, np.random.default_rng(24))[form]
+    kw = {("score_cap" if n == "cap" else n): x for n, x in s.items()}
+    for splits in (0, 2):
+        check(spec, t, on_gpu(spec, t, max_splits=splits, **kw), f"{form} splits {splits}", **s)
 
 
 def test_graph_replays_match_eager():
