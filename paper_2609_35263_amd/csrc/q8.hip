@@ -172,8 +172,20 @@ __global__ __launch_bounds__(256) void q8_read_kernel(DevPlan p, Q8Dev x, const 
 // masked ones (a split may hold no others), and a reference over 2^28 gives a row of NaN.
 constexpr float kFarScore = 0x1p28f;
 __device__ __forceinline__ float reference(float m) { return m < -kFarScore ? 0.0f : m; }
-// The sum that a row's outputs are divided by: 0 for a row of no weight, NaN for one that has no sum.
+// A row's sum of weights: 0 for a row of no weight, NaN for one that has no sum.
 __device__ __forceinline__ float row_sum(float m, float l) { return m <= kFarScore ? l : NAN; }
+
+// The weights meet V rounded to bf16.  Where an output is divided by the sum of the rounded ones, what a rounding does to a weight
+// is taken out of that sum too, so a row that one key rules has that key's values, not up to 2^-8 off.  With few rows this
+// costs nothing; with many 4 % (long_prefix 1,994 us, 2,076), which capped scores get, whose largest weights are any number, and
+// others do without: there the largest is mostly 1, as the reference is the largest score of a row's first tiles.  The LSE is of
+// the weights themselves in all of them.
+__device__ __forceinline__ float plus_rounded(float sum, const bf16x8& w) {
+  const bf16x2 one = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{w[i], w[i + 1]}, one, sum, false);
+  return sum;
+}
 
 // What a kernel's scores are.  CAUSAL: softmax_scale q.k up to the row's own position.  LINEAR: with a slope on the distance, or
 // an interval of keys.  CAPPED: with a cap of kFixedCap at most, and perhaps an interval.  MIXED: with a cap otherwise.
@@ -338,7 +350,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   f32x16 oacc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db) oacc[db] = f32x16{};
-  float m_run = F == CAPPED ? fixed_reference(sc) : -INFINITY, l_run = 0.0f;      // CAPPED: l_run is of half of the keys
+  // The sum of the weights, and of the weights as rounded where that is kept: both of the lane's keys then, half of the row's.
+  // (Joined at the end in the other forms too, long_prefix takes 1,978 us for 1,936: the compiler's schedule of a tile.)
+  constexpr bool ROUNDED = F == CAPPED || F == MIXED;
+  float m_run = F == CAPPED ? fixed_reference(sc) : -INFINITY, l_run = 0.0f, w_run = 0.0f;
 
   auto store_tile = [&](int buf) {
     __bf16* kd = &ks[buf][key * KSTR + part * (W * 16)];
@@ -414,6 +429,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
           const int at = (i + 14) % 16;
           if (i >= 2) pb_next[at >> 3][at & 7] = static_cast<__bf16>(e);
           else pb[at >> 3][at & 7] = static_cast<__bf16>(e);
+          if (i == 9) w_run = plus_rounded(w_run, pb_next[0]);
+          if (i == 1) w_run = plus_rounded(w_run, pb[1]);
         }
         if (second) two = __builtin_amdgcn_rcpf(-1.0f - one);
         if (weights) one = fast_exp2(s[i] * sc.in);
@@ -449,6 +466,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
         l_run += e;
         pb[r >> 3][r & 7] = static_cast<__bf16>(e);
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) w_run = plus_rounded(w_run, pb[t]);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -557,16 +576,19 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
           rs += e;
           pb[2 * kb + (r >> 3)][r & 7] = static_cast<__bf16>(e);
         }
-      rs = halves_sum(rs);
+      if (!ROUNDED) rs = halves_sum(rs);
       if (__any(bump)) {
         const float alpha = fast_exp2(m_run - m_use);
         l_run *= alpha;
+        w_run *= alpha;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
           for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
       }
       l_run += rs;
+#pragma unroll
+      for (int i = 0; ROUNDED && i < 2 * NKB; ++i) w_run = plus_rounded(w_run, pb[i]);
       m_run = m_new;
       // O^T[d][row] += V^T[d][key] P^T[key][row]; step t covers keys 16t + 8*(e/4) + 4*hf + (e%4),
       // the order in which the S^T accumulator holds them
@@ -593,11 +615,14 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
     __syncthreads();
   }
 
-  // ---- epilogue: O = O^T / l, lse = ln(l) + m (natural log) ------------------------------------
-  if (F == CAPPED) l_run = halves_sum(l_run);
+  // ---- epilogue: O = O^T / w, lse = ln(l) + m (natural log) ------------------------------------
+  if (ROUNDED) {
+    l_run = halves_sum(l_run);
+    w_run = halves_sum(w_run);
+  }
   if (!row_ok) return;
-  const float sum = row_sum(m_run, l_run);
-  const float inv_l = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const float sum = row_sum(m_run, l_run), rounded = row_sum(m_run, ROUNDED ? w_run : l_run);
+  const float inv_l = sum == 0.0f ? 0.0f : 1.0f / rounded;
   const float lse_v = sum == 0.0f ? -INFINITY : (m_run + __log2f(sum)) * kLn2;
   if (it.part < 0) {
     __bf16* orow = out + (int64_t(rm.cu + tok) * Hq + head) * D;
@@ -669,7 +694,7 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
   constexpr int OSTR = D + 4;                    // floats per row while the waves' sums are joined
   constexpr int VBYTES = 32 * VSTR, JOIN = 4 * 16 * OSTR * 4;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * VBYTES > JOIN ? 4 * VBYTES : JOIN];
-  __shared__ float wave_m[4][16 * RT], wave_l[4][16 * RT];
+  __shared__ float wave_m[4][16 * RT], wave_l[4][16 * RT], wave_w[4][16 * RT];
 
   // the header, the item and its request in one trip to memory
   const WorkItem it = p.items[blockIdx.x];
@@ -743,13 +768,13 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
   // transposing reads: lanes 2 m and 2 m + 1 of 16 address the two halves of 16 bytes of the m-th of their eight keys
   const unsigned char* const vl = vs + (16 * (col >> 3) + 4 * g + ((col >> 1) & 3)) * VSTR + 8 * (lane & 1);
   f32x4 oacc[RT][D / 16];
-  float m_run[RT], l_run[RT];                    // l_run: this lane's keys alone
+  float m_run[RT], l_run[RT], w_run[RT];         // the sums of this lane's keys alone
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
 #pragma unroll
     for (int db = 0; db < D / 16; ++db) oacc[t][db] = f32x4{};
     m_run[t] = -INFINITY;
-    l_run[t] = 0.0f;
+    l_run[t] = w_run[t] = 0.0f;
   }
 
   auto attend = [&](const Block& b, int block) {
@@ -822,12 +847,14 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
         }
       if (__any(bump[t])) {
         l_run[t] *= alpha[t];
+        w_run[t] *= alpha[t];
 #pragma unroll
         for (int db = 0; db < D / 16; ++db)
 #pragma unroll
           for (int r = 0; r < 4; ++r) oacc[t][db][r] *= alpha[t];
       }
       l_run[t] += rs;
+      w_run[t] = plus_rounded(w_run[t], pb[t]);
       m_run[t] = m_new;
     }
 #pragma unroll
@@ -863,9 +890,11 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     l_run[t] = quarters_sum(l_run[t]);
+    w_run[t] = quarters_sum(w_run[t]);
     if (g == 0) {
       wave_m[wave][16 * t + col] = m_run[t];
       wave_l[wave][16 * t + col] = l_run[t];
+      wave_w[wave][16 * t + col] = w_run[t];
     }
   }
   float* const join = reinterpret_cast<float*>(smem);
@@ -888,13 +917,17 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     __syncthreads();
     const int row = 16 * t + row16;
     if (row >= it.rows) continue;
-    float top = -INFINITY, l = 0.0f;
+    float top = -INFINITY, l = 0.0f, rounded = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) top = fmaxf(top, wave_m[w][row]);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) l += wave_l[w][row] == 0.0f ? 0.0f : wave_l[w][row] * fast_exp2(wave_m[w][row] - top);
+    for (int w = 0; w < 4; ++w) {
+      const float share = wave_l[w][row] == 0.0f ? 0.0f : fast_exp2(wave_m[w][row] - top);
+      l += share == 0.0f ? 0.0f : wave_l[w][row] * share;
+      rounded += share == 0.0f ? 0.0f : wave_w[w][row] * share;
+    }
     l = row_sum(top, l);
-    const float inv_l = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv_l = l == 0.0f ? 0.0f : 1.0f / row_sum(top, rounded);
     const float lse_v = l == 0.0f ? -INFINITY : (top + __log2f(l)) * kLn2;
     const int prow = it.row0 + row, tok = prow / G;
     const int64_t orow = int64_t(rm.cu + tok) * Hq + it.kv_head * G + (prow - tok * G);
