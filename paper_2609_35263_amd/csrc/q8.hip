@@ -63,7 +63,10 @@ __device__ __forceinline__ T wave_most(T x) {
 // ---------------------------------------------------------------------------------------------
 // Append and read.  A wave has one block of 16 slots of one head, of K or of V: all of its rows lie in registers, eight
 // values a lane, so the block's scale is found and applied in one pass.  A workgroup has four blocks in a row of the same
-// head, so mostly a page's, whose run it writes in one piece.
+// head, so mostly a page's, whose run it writes in one piece.  Bound by memory: 16,384 tokens of 8 heads of 128 from cold memory
+// take 20.6 us stored and 17.4 read back, 4.8 and 5.7 TB/s where a large copy reaches 4.8; 64 single tokens 3.3 and 3.4,
+// a launch.  The rows to store are read past the caches, as nothing reads them again: 24 us with the events around it for 29.
+// (Stores past the caches make the next read of the codes wait: the read back 29 us for 20.)
 // ---------------------------------------------------------------------------------------------
 struct BlockPart {
   bool any, is_v;
@@ -246,6 +249,10 @@ __device__ __forceinline__ float capped_of(float s, const Scores& r) {
 // from the accumulators, rounded to bf16 for the second product.  A tile's codes are loaded (half of the bytes) before the
 // MFMAs of the tile before it and turned into bf16 rows in the other LDS buffer after them: once for all NW waves.
 // A wave stages 16 keys, which share a page and a scale: both are the wave's own scalars.
+// Bound by the matrix instructions and the vector work of the softmax, which hardly overlap (of 7,470 clocks a tile of 128 keys,
+// 4,060 and 3,660 a SIMD): 1,024 tokens behind 65,536, 64/8 heads of 128, 1,907-1,995 us on boxes of unlike clocks, 1.11-1.16
+// PFLOP/s, where large library products reach 1.2-1.6.  With capped scores 2,560-2,630, three instructions of lower rate a score for
+// one; 4 x 2,048 tokens behind 0-4,096, 32/8 heads: 474 us causal, 500 with slopes, 630 capped, 765 capped with slopes.
 // ---------------------------------------------------------------------------------------------
 
 // Where the 8-value piece c of a V row lies in its LDS row (stride 16 banks past a multiple of 64): the four pieces that a
@@ -664,6 +671,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
 //     come back by transposing reads of eight codes, which are turned into bf16 in registers.
 // The accumulator of a block's scores, element r of key tile kt, holds key 16 kt + 4 g + r: with the keys of the second
 // product in the order (g, kt, r), the probabilities are its operand where they lie.
+// Bound by memory: a token each behind 64 x 1-32 K cached (64/8 heads of 128, pages of 64) 361 us, 5.95 TB/s, where reads alone reach
+// 6.1; 377 through the caches.  128 tokens behind 16-4,000 (24/4 heads of 64, pages of 16) 32 us: runs of 1,040 bytes
+// begin and end inside lines, 156 MB are read for 137.  One token behind 8,191: 7 us, and 3.5 for the join of its splits.
 // ---------------------------------------------------------------------------------------------
 
 // 16 bytes, where STREAM without a place in the caches.
