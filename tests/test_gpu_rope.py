@@ -267,6 +267,34 @@ def test_a_layers_step_captured_and_replayed():
             assert same(got, want), i
 
 
+def test_overlapping_and_misplaced_buffers_are_refused():
+    """Outputs that share elements with another buffer, strides and addresses that the kernels cannot take: nothing is enqueued."""
+    spec, p, ws = plan(4, 2, 64, [10], [6])
+    r = wp.Rope(rot_dim=64)
+    buf = torch.zeros(6, 40, 64, dtype=torch.bfloat16, device="cuda")
+    q, k, q2, k2 = buf[:, 0:4], buf[:, 4:6], buf[:, 6:10], buf[:, 10:12]
+    wp.rope_apply(r, p, q, k, q2, k2, ws)
+    for a in ((q, k, buf[:, 1:5], k2), (q, k, buf[:, 3:7], k2), (q, k, q2, buf[:, 9:11]), (q, k, q2, buf[:, 3:5]), (q, k, k2.repeat(1, 2, 1), q[:, 1:3])):
+        with pytest.raises(wp.WaveppError) as e:
+            wp.rope_apply(r, p, *a, ws)
+        assert e.value.status == -4, e.value
+    flat = torch.zeros(8000, dtype=torch.bfloat16, device="cuda")
+    other = torch.zeros(6, 4, 64, dtype=torch.bfloat16, device="cuda")
+    for bad in (flat[1:1 + 6 * 256].view(6, 4, 64), flat.as_strided((6, 4, 64), (260, 64, 1)), flat.as_strided((6, 4, 64), (64, 64, 1))):
+        with pytest.raises((wp.WaveppError, ValueError)):
+            wp.rope_apply(r, p, bad, None, other, None, ws)
+    at = torch.zeros(6, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        wp.rope_apply(r, p, q, k, q2, k2, ws, positions=at[:5])
+    with pytest.raises(ValueError):
+        wp.rope_apply(r, p, q, k, q2, k2, ws, positions=at.long())
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        wp.rope_apply(r, p, q, k, q2, k2, ws, stream=side)
+    torch.cuda.synchronize()
+    assert not buf.any()
+
+
 def test_idle_waves_and_overwritten_workspaces():
     spec, p, ws = plan(4, 2, 64, [10, 20], [0, 0])
     x = rows(0, 4, 2, 64)

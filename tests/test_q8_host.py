@@ -115,6 +115,27 @@ def test_a_window_reads_its_window_alone():
     assert items[:, 4].min() == (30001 - 4096) // 128 * 128 and items[:, 5].max() == 30001
 
 
+def rows_of(requests, prefix, chunk, dim=128, page=64, **scores):
+    n = -(-(prefix + chunk) // page)
+    p = wp.q8_plan(num_q_heads=32, num_kv_heads=8, head_dim_qk=dim, head_dim_v=dim, page_size=page, num_pages=n * requests,
+                   softmax_scale=0.1, prefix_lens=[prefix] * requests, chunk_lens=[chunk] * requests,
+                   block_table=np.arange(n * requests).reshape(requests, n), **scores)
+    return p.info()["rows_per_item"]
+
+
+def test_items_of_few_keys_take_four_waves_where_there_are_enough_of_them():
+    assert rows_of(24, 0, 500) == 128                          # short prompts
+    assert rows_of(24, 0, 500, page=16) == 128
+    assert rows_of(4, 2000, 2048) == 256                       # 3,000 keys an item
+    assert rows_of(4, 2000, 2048, dim=64) == 128               # half of the products for each key's turn into bf16
+    assert rows_of(4, 2000, 2048, score_cap=30.0) == 128       # more vector work beside it
+    assert rows_of(4, 8000, 2048, score_cap=30.0) == 256
+    assert rows_of(2, 0, 500) == 256                           # 256 items of 128 rows: not enough
+    begin = np.tile(np.maximum(0, 2000 + np.arange(2048) - 999), 4)
+    assert rows_of(4, 2000, 2048, key_begin=begin) == 128      # a window of 1,000
+    assert rows_of(1, 100000, 2048, key_begin=begin[:2048] + 98000) == 128
+
+
 def call(fn, plan, *bufs, ws=FAKE, size=None):
     size = plan.workspace_bytes if size is None else size
     return getattr(wp.load_library(), fn)(plan.handle, *bufs, ws, size, None)
