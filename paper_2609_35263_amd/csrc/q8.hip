@@ -1027,6 +1027,7 @@ hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto oo = static_cast<__bf16*>(out);
   const int32_t num_many = p.num_items - num_few;
+  if (num_many >= 1 << 23 || num_few >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
   const bool w8 = p.rows_per_item == kGqaRowsPerItem, one = x.few_rows <= 16;
   const Form form = x.cap > 0.0f ? (x.cap <= kFixedCap && !x.slopes ? CAPPED : MIXED) : x.ranges || x.slopes ? LINEAR : CAUSAL;
   if (num_many && !w8 && p.rows_per_item != kGqaRowsPerItem / 2) return hipErrorInvalidValue;

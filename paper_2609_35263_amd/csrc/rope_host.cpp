@@ -40,6 +40,9 @@ struct Rows {
   int64_t stride, width;             // bytes
 };
 
+// The most elements from one token to the next: a wave's 2^30 tokens of them in bytes still lie within 63 bits.
+constexpr int64_t kMostStride = int64_t(1) << 30;
+
 bool positive(double x) { return x > 0.0 && std::isfinite(x); }
 
 }  // namespace
@@ -139,8 +142,8 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
                         Rows{"k_out", reinterpret_cast<uintptr_t>(k_out), k_out_stride, kw}}) {
     if (!r.at) continue;
     if (r.at % 16) return set_error(WAVEPP_EINVAL, "%s must be 16-byte aligned", r.name);
-    if (r.stride < r.width || r.stride % 8 || r.stride > (int64_t(1) << 40))
-      return set_error(WAVEPP_EINVAL, "%s has a stride of %lld elements: a multiple of 8 from %lld on is needed", r.name,
+    if (r.stride < r.width || r.stride % 8 || r.stride > kMostStride)
+      return set_error(WAVEPP_EINVAL, "%s has a stride of %lld elements: a multiple of 8 from %lld to 2^30 is needed", r.name,
                        (long long)r.stride, (long long)r.width);
     rows[n++] = {r.name, r.at, 2 * r.stride, 2 * r.width};
   }

@@ -283,6 +283,14 @@ def test_overlapping_and_misplaced_buffers_are_refused():
     for bad in (flat[1:1 + 6 * 256].view(6, 4, 64), flat.as_strided((6, 4, 64), (260, 64, 1)), flat.as_strided((6, 4, 64), (64, 64, 1))):
         with pytest.raises((wp.WaveppError, ValueError)):
             wp.rope_apply(r, p, bad, None, other, None, ws)
+    lib = wp.load_library()
+    step = buf.stride(0)
+    for stride in (4 * 64 - 8, step + 4, 0, -step, 1 << 31, 1 << 62):
+        for i in range(2):
+            s = [step, step]
+            s[i] = stride
+            assert lib.wavepp_rope_apply(r.handle, p.handle, q.data_ptr(), s[0], None, 0, q2.data_ptr(), s[1], None, 0, None, ws.data_ptr(), ws.nbytes, None) == -1
+            assert b"stride" in lib.wavepp_last_error()
     at = torch.zeros(6, dtype=torch.int32, device="cuda")
     with pytest.raises(ValueError):
         wp.rope_apply(r, p, q, k, q2, k2, ws, positions=at[:5])
