@@ -932,9 +932,10 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     for (int w = 0; w < 4; ++w) top = fmaxf(top, wave_m[w][row]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
+      // a sum of NaN stays so whatever its share, that of a wave which saw no other score included
       const float share = wave_l[w][row] == 0.0f ? 0.0f : fast_exp2(wave_m[w][row] - top);
-      l += share == 0.0f ? 0.0f : wave_l[w][row] * share;
-      rounded += share == 0.0f ? 0.0f : wave_w[w][row] * share;
+      l += wave_l[w][row] * share;
+      rounded += wave_w[w][row] * share;
     }
     l = row_sum(top, l);
     const float inv_l = l == 0.0f ? 0.0f : 1.0f / row_sum(top, rounded);
