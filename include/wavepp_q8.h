@@ -49,7 +49,11 @@ extern "C" {
  * key_begin NULL is 0 and key_end NULL is i + 1 for every query, which is the causal rule.  Both arrays have one entry for
  * each new token, in [0, p_r + c_r]: a window of w keys is key_begin = max(0, i + 1 - w), a document's tokens begin at its
  * first position, and a prefix that all of a request sees ends no earlier than its last position.  A query whose interval
- * is empty sees nothing: its output is zero and its lse -infinity.  Keys in no interval of a tile of queries are not read. */
+ * is empty sees nothing: its output is zero and its lse -infinity.
+ * A tile is up to 256 rows of neighbouring queries of a request, the heads of a KV head's group being rows of their own.  Its
+ * keys are read from the first that one of its queries sees to the last: what lies before or behind may hold any bytes, so
+ * that any page of the pool may stand in the block table for those that every window has left.  Keys between that lie in
+ * none of its queries' intervals are read and have no weight, so they have to be rows that an append stored. */
 typedef struct {
   float cap;
   const float* slopes;

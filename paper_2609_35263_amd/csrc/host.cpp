@@ -825,8 +825,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
                           scores->key_end ? scores->key_end[t] : batch->prefix_lens[r] + i + 1});
       }
   }
-  // Keys of the M rows from r0 on, from a tile's first: all that one of their tokens sees.
-  auto tile_keys = [&](int32_t r, int64_t r0, int64_t M, int64_t KT) {
+  // Keys of the M rows from r0 on: from the first that one of their tokens sees to before the last.
+  auto seen_keys = [&](int32_t r, int64_t r0, int64_t M) {
     const int64_t first = r0 / G, last = (std::min<int64_t>(r0 + M, rows_of(r)) - 1) / G;
     if (!ranged) return TokenRange{0, int32_t(batch->prefix_lens[r] + last + 1)};
     TokenRange u{INT32_MAX, 0};
@@ -834,7 +834,12 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       const TokenRange& x = ranges[size_t(reqs[r].cu + t)];
       if (x.begin < x.end) u = {std::min(u.begin, x.begin), std::max(u.end, x.end)};
     }
-    return u.begin < u.end ? TokenRange{int32_t(u.begin / KT * KT), u.end} : TokenRange{0, 0};
+    return u.begin < u.end ? u : TokenRange{0, 0};
+  };
+  // The same from a tile's first key on.
+  auto tile_keys = [&](int32_t r, int64_t r0, int64_t M, int64_t KT) {
+    const TokenRange u = seen_keys(r, r0, M);
+    return TokenRange{int32_t(u.begin / KT * KT), u.end};
   };
   // Over 8-bit pages, items of few keys also run in the 4-wave form, two workgroups a CU, whose prologues, barriers and
   // diagonals fall beside the other's products; long ones lose more by turning each tile into bf16 for half of the rows.
@@ -1078,7 +1083,7 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     plan->off_blocks = off;
     off = align_up(off + sizeof(Q8Block) * blocks.size(), 16);
     plan->off_item_reqs = off;
-    off = align_up(off + sizeof(ReqMeta) * plan->items.size(), 16);
+    off = align_up(off + sizeof(Q8ItemReq) * plan->items.size(), 16);
     if (ranged) {
       plan->off_ranges = off;
       off = align_up(off + sizeof(TokenRange) * ranges.size(), 16);
@@ -1110,8 +1115,12 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
   if (plan->off_item_reqs) {
     unsigned char* at = plan->blob.data() + plan->off_item_reqs;
     for (const WorkItem& w : plan->items) {
-      if (w.rows > 0) memcpy(at, &reqs[size_t(w.req)], sizeof(ReqMeta));      // (an item of padding has none)
-      at += sizeof(ReqMeta);
+      if (w.rows > 0) {                                                        // (an item of padding has none)
+        const ReqMeta& m = reqs[size_t(w.req)];
+        const Q8ItemReq x{m.prefix, m.cu, m.bt_row, seen_keys(w.req, w.row0, w.rows).begin};
+        memcpy(at, &x, sizeof(x));
+      }
+      at += sizeof(Q8ItemReq);
     }
   }
   if (plan->off_ranges && total)

@@ -22,10 +22,17 @@ struct alignas(16) Q8Block {
   int32_t span;      // new slots of the block: from the low byte to before the next byte
 };
 
+// What a work item needs to know of its request, and the first key that one of its rows sees.  (The last that it loads is the
+// one before its kv_end: kv_begin is a tile's first key, which its rows need not see.)
+struct alignas(16) Q8ItemReq {
+  int32_t prefix, cu, bt_row;        // as in ReqMeta
+  int32_t first;
+};
+
 // What the 8-bit cache's launches need beyond a DevPlan.
 struct Q8Dev {
   const Q8Block* blocks;
-  const ReqMeta* item_reqs;    // of every work item
+  const Q8ItemReq* item_reqs;  // of every work item
   int32_t num_blocks;
   int32_t few_rows;            // most rows of an item that runs with few rows
   bool stream;                 // such items read pages that hardly another reads

@@ -278,13 +278,13 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
 
   // the header, the item and its request in one trip to memory
   const WorkItem it = p.items[blockIdx.x];
-  const ReqMeta rm = x.item_reqs[blockIdx.x];
-  if (int(!meta_ok(p)) | int(it.rows <= 0) | int(rm.chunk <= 0)) return;
+  const Q8ItemReq rm = x.item_reqs[blockIdx.x];
+  if (int(!meta_ok(p)) | int(it.rows <= 0)) return;
   const int Hq = p.num_q_heads, Hkv = p.num_kv_heads;
   const int G = Hq / Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int last = rm.prefix + rm.chunk - 1;                     // the request's last valid position
+  const int last = it.kv_end - 1;                                // the last position to load
   const int32_t* __restrict__ bt = p.bt + rm.bt_row;
   const int B = p.page_size, shift = B == 64 ? 6 : 4;
   const int64_t page_bytes = B * D + kQ8ScaleBytes, page_stride = Hkv * page_bytes;
@@ -292,15 +292,16 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 2 : 1) void attn_q8_kernel(DevPl
   const uint8_t* __restrict__ vpool_h = vpool + it.kv_head * page_bytes;
 
   // ---- K/V tile staging -----------------------------------------------------------------------
-  // Thread tid has a quarter of key tid / 4's row.  Positions past the request's last valid one are clamped to that
-  // one: finite copies that the mask gives zero weight, so stale slots are never read.
+  // Thread tid has a quarter of key tid / 4's row.  Positions past the last that the item's rows see are clamped to that
+  // one, those before the first to that: copies that the mask gives zero weight, so what nobody sees is never read.
   const int key = tid >> 2, part = tid & 3;
   u32x4 kreg[W], vreg[W];
   uint32_t kscale = 0, vscale = 0;
   // The page of this wave's keys is looked up one tile ahead.
-  auto page_of = [&](int tile) { return const_load(bt + (min(tile * KT + wave * 16, last) >> shift)); };
+  auto within = [&](int j) { return min(F == CAUSAL ? j : max(j, rm.first), last); };
+  auto page_of = [&](int tile) { return const_load(bt + (within(tile * KT + wave * 16) >> shift)); };
   auto load_tile = [&](int tile, int page) {
-    const int j = min(tile * KT + key, last), j0 = min(tile * KT + wave * 16, last);
+    const int j = within(tile * KT + key), j0 = within(tile * KT + wave * 16);
     const int64_t at = int64_t(page) * page_stride;
     const uint32_t off = uint32_t(j & (B - 1)) * D + part * (W * 16);
     const uint32_t soff = uint32_t(B * D) + uint32_t((j0 & (B - 1)) >> 4);
@@ -708,13 +709,13 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
 
   // the header, the item and its request in one trip to memory
   const WorkItem it = p.items[blockIdx.x];
-  const ReqMeta rm = x.item_reqs[blockIdx.x];
-  if (int(!meta_ok(p)) | int(it.rows <= 0) | int(rm.chunk <= 0)) return;
+  const Q8ItemReq rm = x.item_reqs[blockIdx.x];
+  if (int(!meta_ok(p)) | int(it.rows <= 0)) return;
   const int Hq = p.num_q_heads, Hkv = p.num_kv_heads;
   const int G = Hq / Hkv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int last = rm.prefix + rm.chunk - 1;     // the request's last valid position
+  const int last = it.kv_end - 1;                // the last position to load
   const int32_t* __restrict__ bt = p.bt + rm.bt_row;
   const int B = p.page_size, shift = B == 64 ? 6 : 4;
   const int64_t page_bytes = B * D + kQ8ScaleBytes, page_stride = Hkv * page_bytes;
@@ -752,25 +753,26 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
     u32x4 k[2][NK], v[NV];
     uint32_t scales;                             // lanes 0..3: K's bytes of both key tiles, V's
   };
-  // Positions past the last valid one are clamped to it, so stale slots are never read.
+  // Positions that no row of the item sees are clamped to those that one does, as above.
+  auto within = [&](int j) { return min(F == CAUSAL ? j : max(j, rm.first), last); };
   auto load = [&](Block& b, int block) {
     const int kbase = 32 * block;
-    const int64_t at[2] = {int64_t(const_load(bt + (kbase >> shift))) * page_stride,
-                           int64_t(const_load(bt + (min(kbase + 16, last) >> shift))) * page_stride};
+    const int64_t at[2] = {int64_t(const_load(bt + (within(kbase) >> shift))) * page_stride,
+                           int64_t(const_load(bt + (within(kbase + 16) >> shift))) * page_stride};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
-      const uint32_t off = uint32_t(min(kbase + 16 * kt + col, last) & (B - 1)) * D + 16 * g;
+      const uint32_t off = uint32_t(within(kbase + 16 * kt + col) & (B - 1)) * D + 16 * g;
 #pragma unroll
       for (int i = 0; i < NK; ++i) b.k[kt][i] = load16<STREAM>(kpool_h + at[kt] + off + 64 * i);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int piece = lane + 64 * i;
-      const uint32_t off = uint32_t(min(kbase + piece / PPR, last) & (B - 1)) * D + 16 * (piece % PPR);
+      const uint32_t off = uint32_t(within(kbase + piece / PPR) & (B - 1)) * D + 16 * (piece % PPR);
       b.v[i] = load16<STREAM>(vpool_h + at[64 * i / D] + off);
     }
     const uint8_t* pool = lane & 2 ? vpool_h : kpool_h;
-    const int j = min(kbase + 16 * (lane & 1), last);
+    const int j = within(kbase + 16 * (lane & 1));
     b.scales = (pool + (lane & 1 ? at[1] : at[0]))[uint32_t(B * D) + uint32_t((j & (B - 1)) >> 4)];
   };
 

@@ -33,7 +33,7 @@ Q8Dev make_q8(const wavepp_plan* plan, void* ws) {
   auto* base = static_cast<unsigned char*>(ws);
   Q8Dev x{};
   x.blocks = reinterpret_cast<const Q8Block*>(base + plan->off_blocks);
-  x.item_reqs = reinterpret_cast<const ReqMeta*>(base + plan->off_item_reqs);
+  x.item_reqs = reinterpret_cast<const Q8ItemReq*>(base + plan->off_item_reqs);
   x.num_blocks = plan->num_blocks;
   x.few_rows = plan->few_rows;
   x.stream = plan->stream;
