@@ -414,8 +414,8 @@ def _current_device():
     if _get_device is None:
         import torch
         # straight to the runtime: the checks in front of it are made here, and cost as much as the call
-        _is_initialized, _get_device = torch.cuda.is_initialized, torch._C._cuda_getDevice
-        _current_stream = torch._C._cuda_getCurrentRawStream
+        _is_initialized, _current_stream = torch.cuda.is_initialized, torch._C._cuda_getCurrentRawStream
+        _get_device = torch._C._cuda_getDevice          # the last one: it tells other threads that all are there
     return _get_device() if _is_initialized() else -2
 
 
