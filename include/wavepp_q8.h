@@ -75,8 +75,9 @@ int wavepp_q8_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, co
  *   k_new [T][num_kv_heads][head_dim], v_new likewise, bf16, 16-byte aligned;
  *   k_pool, v_pool [num_pages][num_kv_heads][wavepp_q8_page_bytes], 16-byte aligned.
  * Written are the codes of the wave's new tokens, the scale bytes of their blocks and, where such a scale grows, the codes
- * of the block's earlier tokens.  Enqueued again on the same rows it leaves the same bytes.  Errors as for
- * wavepp_attn_append_kv. */
+ * of the block's earlier tokens.  Enqueued again on the same rows it leaves the same bytes.  A wave whose blocks of 16 slots
+ * come to 2^25 or more, times num_kv_heads and in whole fours, is WAVEPP_EUNSUPPORTED, here and in wavepp_q8_read_kv.  Errors
+ * otherwise as for wavepp_attn_append_kv. */
 int wavepp_q8_append_kv(const wavepp_plan* plan, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                         void* workspace, size_t ws_bytes, hipStream_t stream);
 
@@ -93,7 +94,9 @@ int wavepp_q8_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
  * Scores under -2^28 ln 2 have no weight; an lse of -infinity says that no key had any, and the output is then zero.  A
  * capped score is off by at most 2^-20 of itself plus, for a cap of 128 or less, 2^-21 of the cap.  With a cap of 50 or
  * less and no slopes, weights of up to 2^65 are summed, so values of V over 2^40 may overflow to infinity.
- * Deterministic: repeated calls give bit-identical results.  Errors as for wavepp_attn_chunked_prefill. */
+ * Deterministic: repeated calls give bit-identical results.  A plan with 2^24 items or more (wavepp_plan_get_info) of requests
+ * of up to 32 rows a KV head, or 2^23 or more of longer ones, is WAVEPP_EUNSUPPORTED.  Errors otherwise as for
+ * wavepp_attn_chunked_prefill. */
 int wavepp_q8_chunked_prefill(const wavepp_plan* plan, const void* q, const void* k_pool, const void* v_pool, void* out,
                               float* lse, void* workspace, size_t ws_bytes, hipStream_t stream);
 

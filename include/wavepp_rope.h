@@ -68,7 +68,8 @@ int wavepp_rope_frequencies(const wavepp_rope* rope, double* out, int32_t capaci
  * position is p_r + i, or positions[its packed index] (device, int32, 4-byte aligned, any value) where positions is not
  * NULL.  rot_offset + rot_dim must not exceed the plan's head_dim_qk.  The workspace holds the plan's upload, as for the
  * other entry points, and is only read.  One launch; it may be captured.  The rope may be destroyed once this returned.
- * Errors: WAVEPP_EINVAL, WAVEPP_EALIAS, WAVEPP_ENOSPACE, WAVEPP_EHIP.  A wave with T = 0 is a no-op. */
+ * A wave of 2^24 tokens or more is WAVEPP_EUNSUPPORTED.
+ * Errors: WAVEPP_EINVAL, WAVEPP_EUNSUPPORTED, WAVEPP_EALIAS, WAVEPP_ENOSPACE, WAVEPP_EHIP.  A wave with T = 0 is a no-op. */
 int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const void* q, int64_t q_stride, const void* k,
                       int64_t k_stride, void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
                       const int32_t* positions, void* workspace, size_t ws_bytes, hipStream_t stream);

@@ -41,6 +41,11 @@ struct Q8Dev {
   float cap;                   // 0: none
 };
 
+// A launch has less than 2^32 threads: so many workgroups at most of the append and the read, which have four waves for four
+// blocks of one head, of K or of V; of attention of few rows, of four waves; and of attention of many, of eight at most.
+constexpr int64_t kQ8MostMoves = (int64_t(1) << 24) - 1, kQ8MostFew = (int64_t(1) << 24) - 1, kQ8MostMany = (int64_t(1) << 23) - 1;
+inline int64_t q8_moves(int32_t num_blocks, int32_t num_kv_heads) { return (int64_t(num_blocks) + 3) / 4 * 2 * num_kv_heads; }
+
 hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new, const void* v_new, void* k_pool,
                             void* v_pool, hipStream_t stream);
 hipError_t launch_q8_read(const DevPlan& p, const Q8Dev& x, const void* k_pool, const void* v_pool, void* k_out, void* v_out,

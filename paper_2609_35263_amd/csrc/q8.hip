@@ -983,15 +983,10 @@ __global__ __launch_bounds__(256, 2) void attn_q8_few_kernel(DevPlan p, Q8Dev x,
 // ---------------------------------------------------------------------------------------------
 // Launchers
 // ---------------------------------------------------------------------------------------------
-namespace {
-// Workgroups of the append and the read: four blocks of one head, of K or of V.
-int64_t move_groups(const DevPlan& p, const Q8Dev& x) { return int64_t((x.num_blocks + 3) / 4) * 2 * p.num_kv_heads; }
-}  // namespace
-
 hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new, const void* v_new, void* k_pool,
                             void* v_pool, hipStream_t stream) {
-  const int64_t groups = move_groups(p, x);
-  if (groups >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
+  const int64_t groups = q8_moves(x.num_blocks, p.num_kv_heads);
+  if (groups > kQ8MostMoves) return hipErrorInvalidValue;
   auto kn = static_cast<const u32x4*>(k_new);
   auto vn = static_cast<const u32x4*>(v_new);
   auto kp = static_cast<uint8_t*>(k_pool);
@@ -1007,8 +1002,8 @@ hipError_t launch_q8_append(const DevPlan& p, const Q8Dev& x, const void* k_new,
 
 hipError_t launch_q8_read(const DevPlan& p, const Q8Dev& x, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                           hipStream_t stream) {
-  const int64_t groups = move_groups(p, x);
-  if (groups >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
+  const int64_t groups = q8_moves(x.num_blocks, p.num_kv_heads);
+  if (groups > kQ8MostMoves) return hipErrorInvalidValue;
   auto kp = static_cast<const uint8_t*>(k_pool);
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto ko = static_cast<bf16x8*>(k_out);
@@ -1030,7 +1025,7 @@ hipError_t launch_q8_attention(const DevPlan& p, const Q8Dev& x, int32_t num_few
   auto vp = static_cast<const uint8_t*>(v_pool);
   auto oo = static_cast<__bf16*>(out);
   const int32_t num_many = p.num_items - num_few;
-  if (num_many >= 1 << 23 || num_few >= 1 << 24) return hipErrorInvalidValue;          // a launch has less than 2^32 threads
+  if (num_many > kQ8MostMany || num_few > kQ8MostFew) return hipErrorInvalidValue;
   const bool w8 = p.rows_per_item == kGqaRowsPerItem, one = x.few_rows <= 16;
   const Form form = x.cap > 0.0f ? (x.cap <= kFixedCap && !x.slopes ? CAPPED : MIXED) : x.ranges || x.slopes ? LINEAR : CAUSAL;
   if (num_many && !w8 && p.rows_per_item != kGqaRowsPerItem / 2) return hipErrorInvalidValue;

@@ -10,14 +10,30 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Whether the launches can have as many workgroups as the wave needs.
+int check_moves(const wavepp_plan* plan) {
+  const int64_t n = q8_moves(plan->num_blocks, plan->shape.num_kv_heads);
+  return n <= kQ8MostMoves ? WAVEPP_OK
+                           : set_error(WAVEPP_EUNSUPPORTED, "the wave touches %d blocks of 16 slots in %d KV heads: store or read it in parts",
+                                       plan->num_blocks, plan->shape.num_kv_heads);
+}
+int check_items(const wavepp_plan* plan) {
+  const int64_t few = plan->num_few, many = int64_t(plan->items.size()) - few;
+  return few <= kQ8MostFew && many <= kQ8MostMany
+             ? WAVEPP_OK
+             : set_error(WAVEPP_EUNSUPPORTED, "the wave has %lld tiles of few rows and %lld of many: plan it in parts", (long long)few,
+                         (long long)many);
+}
+
 // What every call on a plan checks first.  *run: whether there is anything to enqueue.
-int check_call(const wavepp_plan* plan, void* workspace, size_t ws_bytes, bool* run) {
+int check_call(const wavepp_plan* plan, void* workspace, size_t ws_bytes, int (*check_size)(const wavepp_plan*), bool* run) {
   clear_error();
   *run = false;
   if (!plan) return set_error(WAVEPP_EINVAL, "plan is NULL");
   int st = require_cache(plan, Cache::q8);
   if (!st) st = check_workspace(plan, workspace, ws_bytes);
   if (st || plan->total_tokens == 0) return st;
+  if ((st = check_size(plan))) return st;
   *run = true;
   return require_upload(workspace, plan->serial, "wavepp_attn_plan_upload");
 }
@@ -64,7 +80,7 @@ int wavepp_q8_plan(const wavepp_attn_shape* shape, const wavepp_batch* batch, co
 int wavepp_q8_append_kv(const wavepp_plan* plan, const void* k_new, const void* v_new, void* k_pool, void* v_pool,
                         void* workspace, size_t ws_bytes, hipStream_t stream) {
   bool run;
-  int st = check_call(plan, workspace, ws_bytes, &run);
+  int st = check_call(plan, workspace, ws_bytes, check_moves, &run);
   if (st || !run) return st;
   st = check_buffers(k_new, v_new, k_pool, v_pool);
   if (st) return st;
@@ -75,7 +91,7 @@ int wavepp_q8_append_kv(const wavepp_plan* plan, const void* k_new, const void* 
 int wavepp_q8_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v_pool, void* k_out, void* v_out,
                       void* workspace, size_t ws_bytes, hipStream_t stream) {
   bool run;
-  int st = check_call(plan, workspace, ws_bytes, &run);
+  int st = check_call(plan, workspace, ws_bytes, check_moves, &run);
   if (st || !run) return st;
   st = check_buffers(k_pool, v_pool, k_out, v_out);
   if (st) return st;
@@ -86,7 +102,7 @@ int wavepp_q8_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
 int wavepp_q8_chunked_prefill(const wavepp_plan* plan, const void* q, const void* k_pool, const void* v_pool, void* out,
                               float* lse, void* workspace, size_t ws_bytes, hipStream_t stream) {
   bool run;
-  int st = check_call(plan, workspace, ws_bytes, &run);
+  int st = check_call(plan, workspace, ws_bytes, check_items, &run);
   if (st || !run) return st;
   st = check_buffers(q, k_pool, v_pool, out);
   if (st) return st;

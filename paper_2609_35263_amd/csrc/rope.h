@@ -7,6 +7,7 @@
 namespace wavepp {
 
 constexpr int kRopeMaxPairs = 128;
+constexpr int64_t kRopeMaxTokens = (int64_t(1) << 24) - 1;      // a launch has less than 2^32 threads, 256 for a token
 
 // A launch's arguments beside the DevPlan.
 struct RopeDev {

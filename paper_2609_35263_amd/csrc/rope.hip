@@ -192,7 +192,7 @@ Turns<MAX> turns_of(const double* turns, int pairs) {
 }  // namespace
 
 hipError_t launch_rope(const DevPlan& p, const RopeDev& x, const double* turns, hipStream_t stream) {
-  if (p.total_tokens >= 1 << 24) return hipErrorInvalidValue;        // a launch has less than 2^32 threads
+  if (p.total_tokens > kRopeMaxTokens) return hipErrorInvalidValue;
   const int D = p.head_dim_qk, H = (x.q ? p.num_q_heads : 0) + (x.k ? p.num_kv_heads : 0);
   const int copy_q = x.q != x.q_out, copy_k = x.k != x.k_out;
   if (x.offset % 8 || (x.interleaved ? x.pairs % 4 : x.pairs % 8)) {

@@ -40,7 +40,7 @@ struct Rows {
   int64_t stride, width;             // bytes
 };
 
-// The most elements from one token to the next: a wave's 2^30 tokens of them in bytes still lie within 63 bits.
+// The most elements from one token to the next: a call's 2^24 tokens of them in bytes lie well within 63 bits.
 constexpr int64_t kMostStride = int64_t(1) << 30;
 
 bool positive(double x) { return x > 0.0 && std::isfinite(x); }
@@ -130,6 +130,9 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
     return set_error(WAVEPP_EINVAL, "the turned values [%d, %d) exceed the plan's head dim %d", rope->offset,
                      rope->offset + 2 * rope->pairs, int(D));
   if (T == 0) return WAVEPP_OK;
+  if (T > kRopeMaxTokens)
+    return set_error(WAVEPP_EUNSUPPORTED, "the wave has %lld tokens, a call turns %lld at most: plan it in parts", (long long)T,
+                     (long long)kRopeMaxTokens);
   st = require_upload(workspace, plan->serial, "wavepp_attn_plan_upload");
   if (st) return st;
   if (!q != !q_out || !k != !k_out || (!q && !k))
