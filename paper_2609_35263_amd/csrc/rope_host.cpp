@@ -22,11 +22,23 @@ namespace {
 
 constexpr double kTurn = 6.283185307179586476925286766559;
 
+int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b < 0); }
+
+// Whether one of T rows of `w` bytes at b, b + s, ... has a byte of [lo, hi): row j does where j s lies in (lo - b - w, hi - b).
+bool row_meets(int64_t lo, int64_t hi, uintptr_t b, int64_t s, int64_t w, int64_t T) {
+  const int64_t first = floor_div(lo - int64_t(b) - w, s) + 1, last = floor_div(hi - int64_t(b) - 1, s);
+  return std::max<int64_t>(first, 0) <= std::min<int64_t>(last, T - 1);
+}
+
 // Whether two sets of T rows share a byte: rows of `wa` bytes at a, a + sa, ..., and of `wb` at b, b + sb, ...
 bool rows_meet(uintptr_t a, int64_t sa, int64_t wa, uintptr_t b, int64_t sb, int64_t wb, int64_t T) {
   const int64_t d = int64_t(b) - int64_t(a);
   if (d >= (T - 1) * sa + wa || -d >= (T - 1) * sb + wb) return false;        // one ends before the other
-  if (sa != sb) return true;                                                  // rows of unlike strides are not told apart
+  if (sa != sb) {                                                             // row by row: rare, as both lie in each other's gaps
+    for (int64_t i = 0; i < T; ++i)
+      if (row_meets(int64_t(a) + i * sa, int64_t(a) + i * sa + wa, b, sb, wb, T)) return true;
+    return false;
+  }
   // row j of b lies d + (j - i) s from row i of a: whether that is in (-wb, wa) for a difference below T
   const int64_t near = -d / sa;
   for (int64_t k = near - 1; k <= near + 1; ++k)
@@ -133,8 +145,6 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
   if (T > kRopeMaxTokens)
     return set_error(WAVEPP_EUNSUPPORTED, "the wave has %lld tokens, a call turns %lld at most: plan it in parts", (long long)T,
                      (long long)kRopeMaxTokens);
-  st = require_upload(workspace, plan->serial, "wavepp_attn_plan_upload");
-  if (st) return st;
   if (!q != !q_out || !k != !k_out || (!q && !k))
     return set_error(WAVEPP_EINVAL, "q and q_out, and k and k_out, come together, and one of the pairs is needed");
   const int64_t qw = plan->shape.num_q_heads * D, kw = plan->shape.num_kv_heads * D;
@@ -163,6 +173,8 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
     for (int o = n / 2; o < n; ++o)
       if (rows_meet(reinterpret_cast<uintptr_t>(positions), 4, 4, rows[o].at, rows[o].stride, rows[o].width, T))
         return set_error(WAVEPP_EALIAS, "%s and positions overlap", rows[o].name);
+  st = require_upload(workspace, plan->serial, "wavepp_attn_plan_upload");
+  if (st) return st;
   RopeDev x{};
   x.pairs = rope->pairs;
   x.offset = rope->offset;
