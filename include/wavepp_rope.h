@@ -63,9 +63,9 @@ int wavepp_rope_frequencies(const wavepp_rope* rope, double* out, int32_t capaci
 /* Turn the rows of the plan's new tokens.  Device pointers, bf16, 16-byte aligned, rows of a token contiguous:
  *   q, q_out [T][num_q_heads][head_dim_qk], k, k_out [T][num_kv_heads][head_dim_qk];
  * either pair may be NULL as a whole.  A stride is the number of elements from one token to the next: a multiple of 8, at
- * least a token's row and at most 2^30.  So q and k may be slices of one packed projection.  An output is the input itself (same address and
- * stride: in place) or shares no element with any other buffer of the call (else WAVEPP_EALIAS).  A token's
- * position is p_r + i, or positions[its packed index] (device, int32, 4-byte aligned, any value) where positions is not
+ * least a token's row and at most 2^30.  So q and k may be slices of one packed projection.  An output is the input itself
+ * (same address and stride: in place) or shares no element with any other buffer of the call, the positions and what the
+ * workspace holds of the plan among them (else WAVEPP_EALIAS).  A token's position is p_r + i, or positions[its packed index] (device, int32, 4-byte aligned, any value) where positions is not
  * NULL.  rot_offset + rot_dim must not exceed the plan's head_dim_qk.  The workspace holds the plan's upload, as for the
  * other entry points, and is only read.  One launch; it may be captured.  The rope may be destroyed once this returned.
  * A wave of 2^24 tokens or more is WAVEPP_EUNSUPPORTED.

@@ -173,6 +173,10 @@ int wavepp_rope_apply(const wavepp_rope* rope, const wavepp_plan* plan, const vo
     for (int o = n / 2; o < n; ++o)
       if (rows_meet(reinterpret_cast<uintptr_t>(positions), 4, 4, rows[o].at, rows[o].stride, rows[o].width, T))
         return set_error(WAVEPP_EALIAS, "%s and positions overlap", rows[o].name);
+  const int64_t held = int64_t(reinterpret_cast<uintptr_t>(workspace));
+  for (int o = n / 2; o < n; ++o)
+    if (row_meets(held, held + int64_t(plan->meta_bytes), rows[o].at, rows[o].stride, rows[o].width, T))
+      return set_error(WAVEPP_EALIAS, "%s and the plan in the workspace overlap", rows[o].name);
   st = require_upload(workspace, plan->serial, "wavepp_attn_plan_upload");
   if (st) return st;
   RopeDev x{};

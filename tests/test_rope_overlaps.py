@@ -42,3 +42,13 @@ def test_rows_in_each_others_gaps_are_taken():
     assert call(BASE, 4 * WIDTH, BASE + 2 * WIDTH, 8 * WIDTH) == PASSED
     assert call(BASE, 4 * WIDTH, BASE + 2 * WIDTH, 7 * WIDTH) == ALIAS           # the second row of one, the third of the other
     assert call(BASE, 4 * WIDTH, BASE, 8 * WIDTH) == ALIAS
+
+
+def test_an_output_over_the_uploaded_plan_is_refused():
+    """The kernels read the plan from the workspace while they write."""
+    assert call(BASE, WIDTH, WS, WIDTH) == ALIAS
+    assert call(WS, WIDTH, WS, WIDTH) == ALIAS                                   # in place as well
+    assert call(BASE, WIDTH, WS - 2 * WIDTH, WIDTH) == ALIAS
+    assert call(BASE, WIDTH, WS - 12 * WIDTH, WIDTH) == PASSED                   # ends where the workspace begins
+    assert call(BASE, WIDTH, WS + (1 << 20), WIDTH) == PASSED
+    assert call(BASE, WIDTH, WS - 2 * WIDTH, 64 * WIDTH) == PASSED               # rows on both sides of it
