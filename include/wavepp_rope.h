@@ -20,7 +20,7 @@
  *     WAVEPP_ROPE_INDEX   the same with w falling from 1 to 0 with the pair's index: w = 1 - (i - lo) / (hi - lo), kept
  *                         within [0, 1], lo = max(0, floor(at(fast_turns))), hi = min(rot_dim - 1, ceil(at(slow_turns))),
  *                         at(u) = rot_dim ln(original_length / 2 pi u) / (2 ln base); hi - lo is taken as 0.001 at least;
- * or the caller's own.
+ * or the caller's own.  No frequency may lie outside [-1e30, 1e30].
  */
 #ifndef WAVEPP_ROPE_H
 #define WAVEPP_ROPE_H
@@ -48,7 +48,7 @@ typedef struct {
   double original_length;        /* over 0; read by TURNS and INDEX, as are the next two */
   double slow_turns, fast_turns; /* 0 < slow_turns < fast_turns */
   double magnitude;              /* over 0 */
-  const double* frequencies;     /* NULL, or rot_dim / 2 finite numbers (HOST, copied) in place of base and scaling */
+  const double* frequencies;     /* NULL, or rot_dim / 2 numbers (HOST, copied) in place of base and scaling */
 } wavepp_rope_spec;
 
 typedef struct wavepp_rope wavepp_rope;

@@ -57,6 +57,13 @@ constexpr int64_t kMostStride = int64_t(1) << 30;
 
 bool positive(double x) { return x > 0.0 && std::isfinite(x); }
 
+// The largest frequency: at any position of 32 bits its angle is under 2^128 turns, and what fp64 leaves of one after whole
+// turns are taken off, rounded or not before that, is under 2^76: a number of fp32, whose cosine is one too.
+constexpr double kMostFrequency = 1e30;
+int check_frequency(int32_t i, double f) {
+  return std::fabs(f) <= kMostFrequency ? WAVEPP_OK : set_error(WAVEPP_EINVAL, "frequency %d must be a number within [-1e30, 1e30]", i);
+}
+
 }  // namespace
 
 void wavepp_rope::take_turns() {
@@ -84,7 +91,7 @@ int wavepp_rope_create(const wavepp_rope_spec* spec, wavepp_rope** out) {
   rope->magnitude = float(s.magnitude);
   if (s.frequencies) {
     for (int32_t i = 0; i < rope->pairs; ++i) {
-      if (!std::isfinite(s.frequencies[i])) return set_error(WAVEPP_EINVAL, "frequency %d is not finite", i);
+      if (int st = check_frequency(i, s.frequencies[i])) return st;
       rope->frequencies[i] = s.frequencies[i];
     }
     rope->take_turns();
@@ -114,7 +121,7 @@ int wavepp_rope_create(const wavepp_rope_spec* spec, wavepp_rope** out) {
       w = 1.0 - (i - lo) / std::max(hi - lo, 1e-3);
     w = std::min(1.0, std::max(0.0, w));
     rope->frequencies[i] = w == 1.0 ? f : w * f + (1.0 - w) * f / s.factor;
-    if (!std::isfinite(rope->frequencies[i])) return set_error(WAVEPP_EINVAL, "frequency %d is not finite", i);
+    if (int st = check_frequency(i, rope->frequencies[i])) return st;
   }
   rope->take_turns();
   *out = rope.release();
