@@ -89,11 +89,13 @@ int wavepp_q8_read_kv(const wavepp_plan* plan, const void* k_pool, const void* v
 
 /* Attention of the wave's queries over the cached values with the plan's scores, K and V read from 8-bit pages: bf16 q and
  * out, fp32 natural-log lse (or NULL).  bf16 products of the exact cached values with fp32 accumulation, scores and
- * softmax.  A row whose softmax sum is not a number (a NaN in its query, a largest score that overflows or lies beyond
+ * softmax; the weights are rounded to bf16 for their products with V, their sum in the lse is of the weights themselves.
+ * A row whose softmax sum is not a number (a NaN in its query, a largest score that overflows or lies beyond
  * 2^28 ln 2, where fp32 cannot place its exponential) has NaN as its output and its lse, whole or joined from splits.
  * Scores under -2^28 ln 2 have no weight; an lse of -infinity says that no key had any, and the output is then zero.  A
  * capped score is off by at most 2^-20 of itself plus, for a cap of 128 or less, 2^-21 of the cap.  With a cap of 50 or
- * less and no slopes, weights of up to 2^65 are summed, so values of V over 2^40 may overflow to infinity.
+ * less and no slopes, weights of 2^-80 to 2^65 are summed, so values of V over 2^40 may overflow to infinity where scores
+ * lie near the cap, and those under 2^-40 may lose bits where all of a row's scores lie near -cap.
  * Deterministic: repeated calls give bit-identical results.  A plan with 2^24 items or more (wavepp_plan_get_info) of requests
  * of up to 32 rows a KV head, or 2^23 or more of longer ones, is WAVEPP_EUNSUPPORTED.  Errors otherwise as for
  * wavepp_attn_chunked_prefill. */

@@ -173,3 +173,24 @@ def test_a_product_that_overflows_is_a_score_at_the_cap(name):
         ref = reference(spec, t, pools, cap)
         for splits in (1, 3):
             compare(on_gpu(spec, t, max_splits=splits, score_cap=cap), ref, f"{name} cap {cap} splits {splits}")
+
+
+@pytest.mark.parametrize("name", sorted(ALL))
+@pytest.mark.parametrize("sign,power", [(1.0, 40), (-1.0, -40)])
+def test_the_largest_and_smallest_values_beside_scores_at_a_cap_of_50(name, sign, power):
+    """Weights of 2^64 with values of up to 2^40, and weights of 2^-80 with values from 2^-40 on: what the header allows."""
+    spec = wave(name, 141)
+    t = make(spec, 142, garbage=False)
+    t["q"] = ((t["q"].float().abs() + 0.5) * 4000.0 * sign).to(torch.bfloat16)
+    t["k_new"] = t["k_new"].abs() + 0.5
+    d, B = spec.head_dim_qk, spec.page_size
+    t["k_pool"] = torch.from_numpy(oracle.q8.quantise_pool(np.abs(oracle.q8.pool_values(t["k_pool"].numpy(), d, B)) + 0.5))
+    for n in ("v_new", "v_pool"):
+        v = t[n].double().numpy() if n == "v_new" else oracle.q8.pool_values(t[n].numpy(), d, B)
+        # magnitudes between a half and one times the power of two, or from one to two times it where that is the smallest
+        v = np.where(v < 0, -1.0, 1.0) * (0.5 + 0.5 * np.minimum(np.abs(v), 1.0)) * 2.0 ** (power + (power < 0))
+        t[n] = torch.from_numpy(v).to(torch.bfloat16) if n == "v_new" else torch.from_numpy(oracle.q8.quantise_pool(v))
+    pools = appended(spec, t)
+    ref = reference(spec, t, pools, 50.0)
+    for splits in (0, 3):
+        compare(on_gpu(spec, t, max_splits=splits, score_cap=50.0), ref, f"{name} 2^{power}")
