@@ -29,7 +29,9 @@
  * Call order on one stream, per wave: wavepp_q8_plan (host only) -> wavepp_attn_plan_upload -> wavepp_q8_append_kv ->
  * wavepp_q8_chunked_prefill (the last two once per layer, each with its own pools).  The launches of both may be captured
  * into a graph after the upload; its replays run on whatever the buffers then hold.  Calls whose plans have splits write
- * partials into their workspace, so calls that may overlap need a workspace each.
+ * partials into their workspace, so calls that may overlap need a workspace each.  The scores are part of the plan: a model
+ * whose layers differ in theirs, a window here and the whole past there, has a plan, a workspace and an upload a wave for
+ * each kind, and any of them will do for the append.
  */
 #ifndef WAVEPP_Q8_H
 #define WAVEPP_Q8_H

@@ -250,9 +250,9 @@ __device__ __forceinline__ float capped_of(float s, const Scores& r) {
 // MFMAs of the tile before it and turned into bf16 rows in the other LDS buffer after them: once for all NW waves.
 // A wave stages 16 keys, which share a page and a scale: both are the wave's own scalars.
 // Bound by the matrix instructions and the vector work of the softmax, which hardly overlap (of 7,470 clocks a tile of 128 keys,
-// 4,060 and 3,660 a SIMD): 1,024 tokens behind 65,536, 64/8 heads of 128, 1,907-1,995 us on boxes of unlike clocks, 1.11-1.16
+// 4,060 and 3,660 a SIMD): 1,024 tokens behind 65,536, 64/8 heads of 128, 1,896-2,059 us on boxes of unlike clocks, 1.08-1.17
 // PFLOP/s, where large library products reach 1.2-1.6.  With capped scores 2,560-2,630, three instructions of lower rate a score for
-// one; 4 x 2,048 tokens behind 0-4,096, 32/8 heads: 474 us causal, 500 with slopes, 630 capped, 765 capped with slopes.
+// one; 4 x 2,048 tokens behind 0-4,096, 32/8 heads: 474 us causal, 500 with slopes, 630-655 capped, 765 capped with slopes.
 // ---------------------------------------------------------------------------------------------
 
 // Where the 8-value piece c of a V row lies in its LDS row (stride 16 banks past a multiple of 64): the four pieces that a

@@ -150,7 +150,8 @@ __global__ __launch_bounds__(kThreads, 8) void rope_kernel(DevPlan p, RopeDev x,
   }
 }
 
-// Pairs that do not come in whole 16-byte pieces: value by value, a workgroup a token.
+// Pairs that do not come in whole 16-byte pieces: value by value, a workgroup a token.  16,384 tokens of 72 heads of 128: 255 us
+// with 126 values turned from the second on, 333 with 30, bound by the loads and stores of two bytes.
 __global__ __launch_bounds__(kThreads) void rope_any_kernel(DevPlan p, RopeDev x, Turns<kRopeMaxPairs> f, int copy_q, int copy_k) {
   if (!meta_ok(p)) return;
   __shared__ float cs[2][kRopeMaxPairs];
