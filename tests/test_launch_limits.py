@@ -20,8 +20,8 @@ def call(fn, p, n):
 
 def turn(p):
     r = wp.Rope(rot_dim=64)
-    step = p.shape["num_q_heads"] * 64
-    return wp.load_library().wavepp_rope_apply(r.handle, p.handle, FAKE, step, None, 0, FAKE, step, None, 0, None, FAKE, p.workspace_bytes, None)
+    step, rows = p.shape["num_q_heads"] * 64, 1 << 40          # (apart from the workspace)
+    return wp.load_library().wavepp_rope_apply(r.handle, p.handle, rows, step, None, 0, rows, step, None, 0, None, FAKE, p.workspace_bytes, None)
 
 
 @pytest.mark.parametrize("T,status", [((1 << 24) - 64, NOT_UPLOADED), (1 << 24, UNSUPPORTED), ((1 << 24) + 640, UNSUPPORTED)])
