@@ -836,11 +836,9 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     }
     return u.begin < u.end ? u : TokenRange{0, 0};
   };
-  // The same from a tile's first key on.
-  auto tile_keys = [&](int32_t r, int64_t r0, int64_t M, int64_t KT) {
-    const TokenRange u = seen_keys(r, r0, M);
-    return TokenRange{int32_t(u.begin / KT * KT), u.end};
-  };
+  // Where the scores say it, the first such key of every tile of rows of a request, from first_at[request] on.
+  std::vector<int32_t> tile_first;
+  std::vector<size_t> first_at(ranged ? size_t(R) : 0);
   // Over 8-bit pages, items of few keys also run in the 4-wave form, two workgroups a CU, whose prologues, barriers and
   // diagonals fall beside the other's products; long ones lose more by turning each tile into bf16 for half of the rows.
   // With mean keys an item of (us with 8 waves, with 4), 32/8 heads of 128: 300 137, 126; 800 243, 237; 1,250 181, 175;
@@ -854,8 +852,8 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       const int64_t rows = rows_of(r);
       items += ceil_div(rows, kGqaRowsPerItem / 2) * s.num_kv_heads;
       for (int64_t r0 = 0; r0 < rows; r0 += kGqaRowsPerItem, ++tiles) {
-        const TokenRange k = tile_keys(r, r0, kGqaRowsPerItem, kKvTile);
-        keys += k.end - k.begin;
+        const TokenRange k = seen_keys(r, r0, kGqaRowsPerItem);
+        keys += k.end - k.begin / kKvTile * kKvTile;
       }
     }
     const int64_t most = (scores && scores->cap > 0.0f ? 4096 : 1536) * (128 / s.head_dim_qk);
@@ -882,7 +880,12 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
       const int64_t rows_total = rows_of(r);
       if (few_rows) plan->few_rows = std::max(plan->few_rows, int32_t(rows_total));
       seen.clear();
-      for (int64_t r0 = 0; r0 < rows_total; r0 += M) seen.push_back(tile_keys(r, r0, M, KT));
+      if (ranged) first_at[size_t(r)] = tile_first.size();
+      for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
+        const TokenRange u = seen_keys(r, r0, M);
+        seen.push_back({int32_t(u.begin / KT * KT), u.end});
+        if (ranged) tile_first.push_back(u.begin);
+      }
       for (int32_t g = 0; g < s.num_kv_heads; ++g)
         for (int64_t r0 = 0; r0 < rows_total; r0 += M) {
           WorkItem w{};
@@ -1126,7 +1129,9 @@ int plan_wave(const wavepp_attn_shape* shape, const wavepp_batch* batch, int32_t
     for (const WorkItem& w : plan->items) {
       if (w.rows > 0) {                                                        // (an item of padding has none)
         const ReqMeta& m = reqs[size_t(w.req)];
-        const Q8ItemReq x{m.prefix, m.cu, m.bt_row, seen_keys(w.req, w.row0, w.rows).begin};
+        // (a request of few rows has one tile, which begins with its first)
+        const int32_t first = ranged ? tile_first[first_at[size_t(w.req)] + size_t(w.row0 / plan->rows_per_item)] : 0;
+        const Q8ItemReq x{m.prefix, m.cu, m.bt_row, first};
         memcpy(at, &x, sizeof(x));
       }
       at += sizeof(Q8ItemReq);
